@@ -50,6 +50,25 @@ class McdOuterConfig(ctypes.Structure):
                 ("temperature", ctypes.c_float), ("seed", ctypes.c_uint64)]
 
 
+class McdPagedKV(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class McdChunks(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("cached", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32), ("max_tokens", ctypes.c_int32)]
+
+
+class McdRope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("scale", ctypes.c_float), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
 CALL_TRACE_DTYPE = np.dtype([("a", "<i4"), ("n_rows", "<i4"), ("pos0", "<i4"), ("n_drafts", "<i4"),
                              ("input_ids", "<i4", 8), ("drafts", "<i4", 8), ("n_acc", "<i4"),
                              ("n_emit", "<i4"), ("emitted", "<i4", 8), ("n_next", "<i4"),
@@ -123,6 +142,14 @@ def load_library() -> ctypes.CDLL:
         "mcd_tc_gemm": (I32, [I32, I32, I32, I32, P, P, P, P]),
         "mcd_tc_tile": (I32, [I32, I32, I32, P, P, P]),
         "mcd_tc_gemm_tiled": (I32, [I32, I32, I32, I32, P, P, P, P, P]),
+        "mcd_rope_freqs": (I32, [I32, I32, ctypes.c_double, ctypes.c_double, I32, ctypes.c_double, ctypes.c_double,
+                                 P, P]),
+        "mcd_rope_append": (I32, [P, I32, P, I32, P, I64, I32, P, I64, P, P, P, P, ctypes.c_float, P, P]),
+        "mcd_paged_attention": (I32, [P, I32, P, I32, P, I64, P, I64, ctypes.c_float, P, I32, P, I64, P, P]),
+        "mcd_paged_attention_workspace": (I64, [P, P, I32]),
+        "mcd_pages_fork": (I32, [P, P, P, I32, P, I32, P, I32, P, P, P, I32, P, I32, P, I64, P, P]),
+        "mcd_pages_fork_workspace": (I64, [I32, I32, I32]),
+        "mcd_pages_compact": (I32, [P, I32, P, P, I32, P, P, I32, P, P, P, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -300,6 +327,155 @@ def mcd_tc_gemm_tiled(M: int, N: int, K: int, bn: int, A_tiled, B_tiled, Y, err,
     _check("mcd_tc_gemm_tiled", load_library().mcd_tc_gemm_tiled(
         M, N, K, bn, _ptr(A_tiled), _ptr(B_tiled), _ptr(Y), _ptr(err),
         ctypes.c_void_p(stream.cuda_stream if stream is not None else None)))
+
+
+# ---- paged cache (include/mcd_cache.h) ---------------------------------------------------
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
+
+
+def _stream(stream) -> Optional[int]:
+    return stream.cuda_stream if stream is not None else None
+
+
+def _kv_dtype(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("rows and pages are float32 or bfloat16")
+    return 0 if t.dtype == torch.float32 else 1      # MCD_WEIGHT_F32 / MCD_WEIGHT_BF16
+
+
+def _i32(t, what: str, shape=None):
+    """An int32 device tensor whose rows are read one after another."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: a contiguous int32 tensor" + ("" if shape is None else f" of shape {tuple(shape)}"))
+    return _ptr(t)
+
+
+def _f32(t, what: str, n: int):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what}: {n} contiguous float32 values")
+    return _ptr(t)
+
+
+def paged_kv(k, v) -> McdPagedKV:
+    """Descriptor of a page pool: k and v device tensors [layers, pages, kv heads, page size, head dim]
+    (float32 or bfloat16) of the same shape and strides, the last dimension contiguous.  It keeps them."""
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(4) != 1:
+        raise ValueError("k and v: [layers, pages, kv heads, page size, head dim] alike, the last dimension contiguous")
+    st = k.stride()
+    d = McdPagedKV(_ptr(k), _ptr(v), st[0], st[1], st[2], st[3], *k.shape, _kv_dtype(k))
+    d.kept = (k, v)
+    return d
+
+
+def chunks(table, cached, row_start, n_rows: int, max_rows: int, max_tokens: int) -> McdChunks:
+    """Descriptor of a call's new rows: table int32 [sequences, columns], cached int32 [sequences], row_start
+    int32 [sequences + 1], all on the device; the rest are host bounds.  It keeps them."""
+    n = cached.numel()
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("table: [sequences, columns]")
+    d = McdChunks(_i32(table, "table"), _i32(cached, "cached"), _i32(row_start, "row_start", (n + 1,)), n, table.shape[1], n_rows,
+                  max_rows, max_tokens)
+    d.kept = (table, cached, row_start)
+    return d
+
+
+def rope(inv_freq=None, rot_dim: int = 0, interleaved: bool = False, scale: float = 1.0) -> McdRope:
+    """Descriptor of a rotation: inv_freq float64 [rot_dim / 2] on the device; rot_dim 0: none."""
+    import torch
+    if rot_dim and (inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or inv_freq.numel() != rot_dim // 2):
+        raise ValueError("inv_freq: rot_dim / 2 contiguous float64 values")
+    d = McdRope(_ptr(inv_freq) if rot_dim else None, scale, rot_dim, int(interleaved))
+    d.kept = inv_freq
+    return d
+
+
+def mcd_rope_freqs(rot_dim: int, base: float, kind: int = ROPE_PLAIN, factor: float = 1.0, train_tokens: int = 0,
+                   beta_fast: float = 32.0, beta_slow: float = 1.0) -> Tuple[np.ndarray, float]:
+    """(frequencies float64 [rot_dim / 2], scale) of the named kind; on the host."""
+    out = np.zeros(max(rot_dim // 2, 1), dtype=np.float64)
+    scale = ctypes.c_float()
+    _check("mcd_rope_freqs", load_library().mcd_rope_freqs(kind, rot_dim, base, factor, train_tokens, beta_fast,
+                                                           beta_slow, out.ctypes.data, ctypes.addressof(scale)))
+    return out, float(scale.value)
+
+
+def _rows(t, what: str, n_rows: int, width: int) -> int:
+    """Row stride (elements) of a packed row buffer whose rows hold `width` contiguous elements."""
+    st, row = t.stride(), 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(st[1:])):
+        if size != 1 and stride != row:
+            raise ValueError(f"{what}: a row's elements are contiguous")
+        row *= size
+    if t.shape[0] < n_rows or row < width:
+        raise ValueError(f"{what}: at least {n_rows} rows of {width} elements")
+    return st[0] if t.shape[0] > 1 else row
+
+
+def mcd_rope_append(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: int, qkv, q_out, rot: McdRope, err,
+                    positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
+    """New rows' q | k | v (qkv [rows, (q + 2 kv heads) * head dim]) normalised, rotated, written to q_out
+    [rows, q heads * head dim] (the cache's type) and to the pages of `layer`; asynchronous."""
+    d = kv.head_dim
+    if _kv_dtype(q_out) != kv.dtype:
+        raise ValueError("q_out has the cache's type")
+    _check("mcd_rope_append", load_library().mcd_rope_append(
+        ctypes.addressof(kv), layer, ctypes.addressof(ch), n_q_heads, _ptr(qkv),
+        _rows(qkv, "qkv", ch.n_rows, (n_q_heads + 2 * kv.n_kv_heads) * d), _kv_dtype(qkv), _ptr(q_out),
+        _rows(q_out, "q_out", ch.n_rows, n_q_heads * d), ctypes.addressof(rot), _i32(positions, "positions", (ch.n_rows,)),
+        _f32(q_norm, "q_norm", d), _f32(k_norm, "k_norm", d), eps, _i32(err, "err"), _stream(stream)))
+
+
+def mcd_paged_attention_workspace(kv: McdPagedKV, ch: McdChunks, n_q_heads: int) -> int:
+    return int(load_library().mcd_paged_attention_workspace(ctypes.addressof(kv), ctypes.addressof(ch), n_q_heads))
+
+
+def mcd_paged_attention(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: int, q, out, scale: float, workspace, err,
+                        mask=None, stream=None):
+    """out [rows, q heads * head dim] = attention of the new rows q over the pages of `layer`, causal, or among the new
+    rows as the bits of mask (int32 [rows, words]) say; workspace: uint8, mcd_paged_attention_workspace
+    bytes, or None where that is 0.  Asynchronous."""
+    w = n_q_heads * kv.head_dim
+    if _kv_dtype(q) != kv.dtype or _kv_dtype(out) != kv.dtype:
+        raise ValueError("q and out have the cache's type")
+    if mask is not None and (mask.dim() != 2 or mask.shape[0] < ch.n_rows):
+        raise ValueError("mask: [rows, words]")
+    _check("mcd_paged_attention", load_library().mcd_paged_attention(
+        ctypes.addressof(kv), layer, ctypes.addressof(ch), n_q_heads, _ptr(q), _rows(q, "q", ch.n_rows, w), _ptr(out),
+        _rows(out, "out", ch.n_rows, w), scale, _i32(mask, "mask"), 0 if mask is None else mask.shape[1], _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _i32(err, "err"), _stream(stream)))
+
+
+def mcd_pages_fork_workspace(n_src: int, table_out) -> int:
+    return int(load_library().mcd_pages_fork_workspace(n_src, *table_out.shape))
+
+
+def mcd_pages_fork(kv: McdPagedKV, ref_in, ref_out, table_in, len_in, parent, table_out, len_out, workspace, err,
+                   reserve=None, release: bool = False, stream=None):
+    """Sequences of table_out from those of table_in (int32 device tensors throughout); asynchronous."""
+    n_src, src_cols = table_in.shape
+    n_dst, dst_cols = table_out.shape
+    _check("mcd_pages_fork", load_library().mcd_pages_fork(
+        ctypes.addressof(kv), _i32(ref_in, "ref_in", (kv.n_pages,)), _i32(ref_out, "ref_out", (kv.n_pages,)), n_src,
+        _i32(table_in, "table_in"), src_cols, _i32(len_in, "len_in", (n_src,)), n_dst, _i32(parent, "parent", (n_dst,)),
+        _i32(reserve, "reserve", (n_dst,)), _i32(table_out, "table_out"), dst_cols, _i32(len_out, "len_out", (n_dst,)), int(release),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _i32(err, "err"), _stream(stream)))
+
+
+def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, len_out, err, stream=None):
+    """Kept tokens of every sequence moved together, in all layers (int32 device tensors throughout; len_out may be
+    None); asynchronous."""
+    n, cols = table_in.shape
+    _check("mcd_pages_compact", load_library().mcd_pages_compact(
+        ctypes.addressof(kv), n, _i32(table_in, "table_in"), _i32(table_out, "table_out", (n, cols)), cols,
+        _i32(start, "start", (n,)), _i32(keep, "keep", (n, keep.shape[1])), keep.shape[1], _i32(n_keep, "n_keep", (n,)),
+        _i32(len_out, "len_out", (n,)), _i32(err, "err"), _stream(stream)))
 
 
 def mcd_status_str(status: int) -> str:
