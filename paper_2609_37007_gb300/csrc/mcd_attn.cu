@@ -9,6 +9,8 @@
 // The query vectors of one KV head (its group of query heads x the sequence's new rows, "packed"
 // vector p = row * group + head of the group) read the same keys, so a CTA takes a tile of packed vectors
 // of one (sequence, KV head).
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "mcd_cache.cuh"
@@ -26,6 +28,8 @@ struct AttnArgs {
   int* err;
   long long q_stride, out_stride;
   int layer, group, mask_words;
+  int splits;              // parts of a sequence's keys
+  float* part;             // workspace of the parts (null: the CTAs of a cluster join them)
   float c;                 // scale * log2(e)
 };
 
@@ -49,12 +53,12 @@ __device__ __forceinline__ long long key_at(const AttnArgs& a, int s, int h, int
          pos % a.kv.page_size * a.kv.token_stride;
 }
 
-// ---- plain fp32 arithmetic -------------------------------------------------------------------------
-// A CTA of 16 x 16 threads takes 16 RM packed vectors against tiles of 64 keys: thread (ty, tx) has rows
-// ty RM .. and keys tx + 16 c of the scores, then dimensions 4 tx .. (+ 64) of the same rows of o.
-// The probabilities pass between the 16 threads of a row through shared memory.
-constexpr int kFN = 64;
-constexpr int kFThreads = 256;
+// 2^x by the hardware's approximation (relative error 2^-22).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 template <class T>
 __device__ __forceinline__ float4 load4(const T* p);
@@ -70,9 +74,61 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
 }
 
+// Output element of packed vector p, dimension d.
+template <class T, int D>
+__device__ __forceinline__ T* out_at(const AttnArgs& a, const Seq& q, int h, long long p, int d) {
+  return static_cast<T*>(a.out) + (q.row0 + p / a.group) * a.out_stride + (h * a.group + p % a.group) * D + d;
+}
+
+// Part z of the keys [0, n_keys), in whole tiles of `tile` keys.
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span part_of(int n_keys, int z, int splits, int tile) {
+  const int per = ((n_keys + splits - 1) / splits + tile - 1) / tile * tile;
+  const long long lo = min((long long)z * per, (long long)n_keys);
+  return {(int)lo, (int)min((long long)n_keys, lo + per)};
+}
+
+// Joins the parts of `vecs` packed vectors (from p0 on) that the CTAs of a cluster hold in the same places of their shared
+// memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
+// m = -inf and l = 0; nothing at all gives zeros.
+template <class T, int D>
+__device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, long long p0, int vecs, float* o, int pitch,
+                                             float* m, float* l) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cl = cg::this_cluster();
+  cl.sync();
+  const int n = (int)cl.num_blocks(), threads = (int)blockDim.x;
+  for (int t = (int)cl.block_rank() * threads + threadIdx.x; t < vecs * (D / 4); t += n * threads) {
+    const int r = t / (D / 4), d = t % (D / 4) * 4;
+    float mx = -INFINITY;
+    for (int z = 0; z < n; ++z) mx = fmaxf(mx, *cl.map_shared_rank(m + r, z));
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z = 0; z < n; ++z) {
+      const float w = exp2f(*cl.map_shared_rank(m + r, z) - base);
+      const float4 y = *reinterpret_cast<const float4*>(cl.map_shared_rank(o + r * pitch + d, z));
+      sum = fmaf(w, *cl.map_shared_rank(l + r, z), sum);
+      x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    store4(out_at<T, D>(a, q, h, p0 + r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+  }
+  cl.sync();                                           // nobody leaves while others read
+}
+
+// ---- plain fp32 arithmetic -------------------------------------------------------------------------
+// A CTA of 16 x 16 threads takes 16 RM packed vectors against tiles of 64 keys: thread (ty, tx) has rows
+// ty RM .. and keys tx + 16 c of the scores, then dimensions 4 tx .. (+ 64) of the same rows of o.
+// The probabilities pass between the 16 threads of a row through shared memory.
+constexpr int kFN = 64;
+constexpr int kFThreads = 256;
+
 template <int D, int RM>
 struct FSmem {
-  float q[16 * RM][D + 4], k[kFN][D + 4], v[kFN][D], p[16 * RM][kFN + 4];
+  float q[16 * RM][D + 4], k[kFN][D + 4], v[kFN][D], p[16 * RM][kFN + 4], m[16 * RM], l[16 * RM];
 };
 
 template <class T, int D, int RM>
@@ -86,10 +142,11 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
   tc::pdl_trigger();
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
-  const long long vecs = (long long)max(q.n, 0) * a.group, p0 = (long long)blockIdx.x * kBM;
-  if (p0 >= vecs) return;
+  const int z = blockIdx.x % a.splits;
+  const long long vecs = (long long)max(q.n, 0) * a.group, p0 = (long long)(blockIdx.x / a.splits) * kBM;
+  if (p0 >= vecs) return;                              // (all CTAs of the cluster alike)
   const int last_row = (int)min((long long)q.n - 1, (p0 + kBM - 1) / a.group);
-  const int n_keys = a.mask ? q.cached + q.n : q.cached + last_row + 1;
+  const Span keys = part_of(a.mask ? q.cached + q.n : q.cached + last_row + 1, z, a.splits, kFN);
 
   for (int i = threadIdx.x; i < kBM * (D / 4); i += kFThreads) {
     const int r = i / (D / 4), d = i % (D / 4) * 4;
@@ -108,12 +165,12 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < kDC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  for (int k0 = 0; k0 < n_keys; k0 += kFN) {
+  for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
     __syncthreads();
     for (int i = threadIdx.x; i < kFN * (D / 4); i += kFThreads) {
       const int r = i / (D / 4), d = i % (D / 4) * 4;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-      if (k0 + r < n_keys) {
+      if (k0 + r < keys.hi) {
         const long long at = key_at(a, s, h, k0 + r);
         if (at >= 0) {
           x = load4(static_cast<const T*>(a.kv.k) + at + d);
@@ -124,11 +181,11 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       *reinterpret_cast<float4*>(&sm.v[r][d]) = y;
     }
     __syncthreads();
-    float z[RM][4];
+    float sc[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) z[r][c] = 0.f;
+      for (int c = 0; c < 4; ++c) sc[r][c] = 0.f;
 #pragma unroll 4
     for (int d = 0; d < D; d += 4) {
       float4 kk[4];
@@ -139,7 +196,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
         const float4 qq = *reinterpret_cast<const float4*>(&sm.q[ty * RM + r][d]);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          z[r][c] = fmaf(qq.x, kk[c].x, fmaf(qq.y, kk[c].y, fmaf(qq.z, kk[c].z, fmaf(qq.w, kk[c].w, z[r][c]))));
+          sc[r][c] = fmaf(qq.x, kk[c].x, fmaf(qq.y, kk[c].y, fmaf(qq.z, kk[c].z, fmaf(qq.w, kk[c].w, sc[r][c]))));
       }
     }
     const bool edge = k0 + kFN > q.cached;             // some key of the tile may be hidden from some row
@@ -151,8 +208,8 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         see[c] = !edge || sees(a, q, row, k0 + tx + 16 * c);
-        z[r][c] = see[c] ? z[r][c] * a.c : -INFINITY;
-        mx = fmaxf(mx, z[r][c]);
+        sc[r][c] = see[c] ? sc[r][c] * a.c : -INFINITY;
+        mx = fmaxf(mx, sc[r][c]);
       }
 #pragma unroll
       for (int w = 8; w; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
@@ -160,7 +217,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       float sum = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const float p = exp2f(z[r][c] - base);
+        const float p = exp2f(sc[r][c] - base);
         sum += see[c] ? p : 0.f;
         sm.p[ty * RM + r][tx + 16 * c] = see[c] ? p : -0.f;      // (hidden: the sign says so)
       }
@@ -170,7 +227,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       for (int c = 0; c < kDC; ++c) o[r][c].x *= f, o[r][c].y *= f, o[r][c].z *= f, o[r][c].w *= f;
     }
     __syncwarp();
-    const int nk = min(kFN, n_keys - k0);
+    const int nk = min(kFN, keys.hi - k0);
     for (int j = 0; j < nk; ++j) {
       float4 vv[kDC];
 #pragma unroll
@@ -191,17 +248,356 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
   }
 #pragma unroll
   for (int r = 0; r < RM; ++r) {
-    float sum = l[r];
 #pragma unroll
-    for (int w = 8; w; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+    for (int w = 8; w; w >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], w);
+  }
+  if (a.splits > 1) {
+    __syncthreads();                                   // the last tile has been read
+    float(&os)[kFN][D + 4] = sm.k;
+    static_assert(kBM <= kFN, "o takes the place of the keys");
+#pragma unroll
+    for (int r = 0; r < RM; ++r) {
+#pragma unroll
+      for (int c = 0; c < kDC; ++c) *reinterpret_cast<float4*>(&os[ty * RM + r][tx * 4 + 64 * c]) = o[r][c];
+      if (tx == 0) sm.m[ty * RM + r] = m[r], sm.l[ty * RM + r] = l[r];
+    }
+    join_cluster<T, D>(a, q, h, p0, (int)min((long long)kBM, vecs - p0), &os[0][0], D + 4, sm.m, sm.l);
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < RM; ++r) {
     const long long p = p0 + ty * RM + r;
     if (p >= vecs) continue;
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const float f = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
     for (int c = 0; c < kDC; ++c)
-      store4(static_cast<T*>(a.out) + (q.row0 + p / a.group) * a.out_stride + (h * a.group + p % a.group) * D + tx * 4 + 64 * c,
-             make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
+      store4(out_at<T, D>(a, q, h, p, tx * 4 + 64 * c), make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
   }
+}
+
+// ---- up to 16 packed vectors of a KV head, bf16 ------------------------------------------------------------
+// Reading K and V once is all there is to do (4 * 16 flop a byte at most), so the tile is built for loads:
+// four warps share tiles of 64 keys that travel through a ring of cp.async stages; warp w multiplies
+// its 16 keys with the 16 vectors on mma.m16n8k16 (scores: vectors x keys; o: vectors x dimensions) and
+// keeps a maximum, a sum and an o of its own, joined at the end.  Probabilities are multiplied as a hi + lo
+// pair of bf16 (16 bits): the second product costs nothing next to the loads.
+// Rows of a stage hold D bf16 in 16-byte chunks, chunk c at c ^ (row % 8): ldmatrix without conflicts.
+constexpr int kSTile = 64, kSThreads = 128, kSVecs = 16;
+template <int D>
+struct SLayout {
+  static constexpr int kHalf = kSTile * D * 2, kStage = 2 * kHalf;      // K, then V
+  static constexpr int kStages = D == 128 ? 3 : 5;
+  static constexpr int kBytes = kStages * kStage;
+  static constexpr int kPitch = D + 4;
+  static_assert(4 * kSVecs * kPitch * 4 <= kBytes, "the warps' o takes the stages' place");
+};
+__device__ __forceinline__ void cpa16_or_zero(void* dst, const void* src, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ bool bf16x2_finite(uint32_t w) {
+  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) {
+  using L = SLayout<D>;
+  constexpr int kC = D / 8;                            // chunks of a row
+  constexpr int kRows = kSThreads / kC;                // rows a pass of the copies takes: 8 or 16
+  extern __shared__ __align__(128) uint8_t s_smem[];
+  __shared__ float sm_m[4][kSVecs], sm_l[4][kSVecs], fin_m[kSVecs], fin_l[kSVecs];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int h = blockIdx.y, s = blockIdx.z, split = blockIdx.x;
+  tc::pdl_wait();
+  tc::pdl_trigger();
+  const Seq q = load_seq(a.ch, s);
+  if (q.n < 0 && split == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
+  if (q.n <= 0 || q.n > kSVecs / a.group) return;      // (more: the chunk kernel's)
+  const int vecs = q.n * a.group;
+  const Span keys = part_of(q.cached + q.n, split, a.splits, kSTile);
+  const int n_tiles = (keys.hi - keys.lo + kSTile - 1) / kSTile;
+
+  const uint16_t* kp = static_cast<const uint16_t*>(a.kv.k) + a.layer * a.kv.layer_stride + h * a.kv.head_stride;
+  const uint16_t* vp = static_cast<const uint16_t*>(a.kv.v) + a.layer * a.kv.layer_stride + h * a.kv.head_stride;
+  const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
+  const int chunk = threadIdx.x % kC, sub = threadIdx.x / kC;
+  // pages of the four 16-key groups of tile t (16 keys lie in one page)
+  auto pages_of = [&](int t, int (&pg)[4]) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int pos = keys.lo + t * kSTile + 16 * g;
+      pg[g] = t < n_tiles && pos < keys.hi ? __ldg(table + pos / a.kv.page_size) : 0;
+    }
+  };
+  auto copy_tile = [&](int t, const int (&pg)[4]) {
+    if (t < n_tiles) {
+      uint8_t* st = s_smem + t % L::kStages * L::kStage;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int pos0 = keys.lo + t * kSTile + 16 * g;
+        const bool ok = pg[g] >= 0 && pg[g] < a.kv.n_pages;
+        if (!ok && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
+        const long long base = ok ? pg[g] * a.kv.page_stride + pos0 % a.kv.page_size * a.kv.token_stride : 0;
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += kRows) {
+          const int r = r0 + sub, row = 16 * g + r;
+          const bool real = ok && pos0 + r < keys.hi;
+          const long long off = real ? base + r * a.kv.token_stride + chunk * 8 : 0;
+          const int at = row * (D * 2) + ((chunk ^ (row & 7)) << 4);
+          cpa16_or_zero(st + at, kp + off, real);
+          cpa16_or_zero(st + L::kHalf + at, vp + off, real);
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  int pg[4];
+  pages_of(0, pg);
+  copy_tile(0, pg);
+#pragma unroll
+  for (int t = 1; t < L::kStages - 1; ++t) {
+    pages_of(t, pg);
+    copy_tile(t, pg);
+  }
+  pages_of(L::kStages - 1, pg);
+
+  // the vectors as A fragments: rows lane / 4 and + 8, columns 2 (lane % 4) and + 8 of every 16
+  uint4 qf[D / 16];
+  const int r0 = lane >> 2, r1 = r0 + 8;
+  {
+    auto ptr = [&](int p) {
+      return static_cast<const uint16_t*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + 2 * (lane & 3);
+    };
+    const uint16_t *q0 = ptr(min(r0, vecs - 1)), *q1 = ptr(min(r1, vecs - 1));
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      qf[i].x = __ldg(reinterpret_cast<const uint32_t*>(q0 + 16 * i));
+      qf[i].y = __ldg(reinterpret_cast<const uint32_t*>(q1 + 16 * i));
+      qf[i].z = __ldg(reinterpret_cast<const uint32_t*>(q0 + 16 * i + 8));
+      qf[i].w = __ldg(reinterpret_cast<const uint32_t*>(q1 + 16 * i + 8));
+    }
+  }
+  float o[D / 8][4];
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+  // rows of the vectors (none: nobody reads what such a vector gives)
+  const int i0 = r0 < vecs ? r0 / a.group : -1, i1 = r1 < vecs ? r1 / a.group : -1;
+
+  for (int t = 0; t < n_tiles; ++t) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
+    __syncthreads();                                   // tile t is in; tile t - 1 has been read
+    copy_tile(t + L::kStages - 1, pg);
+    pages_of(t + L::kStages, pg);
+    const uint32_t ks = smem_u32(s_smem + t % L::kStages * L::kStage), vs = ks + L::kHalf;
+    const int key0 = keys.lo + t * kSTile + 16 * warp;
+    float z[2][4] = {};
+    {
+      const int row = 16 * warp + (lane & 7) + ((lane & 16) >> 1);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t b[4];
+        ldsm4(b, ks + row * (D * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+        mma_bf16_16816(z[0], qf[i], b[0], b[1]);
+        mma_bf16_16816(z[1], qf[i], b[2], b[3]);
+      }
+    }
+    const bool edge = key0 + 16 > q.cached;
+    unsigned hidden = 0;                               // bit 4 n + e: z[n][e] is hidden
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = e < 2 ? i0 : i1;
+          if (i >= 0 && !sees(a, q, i, key0 + 8 * n + 2 * (lane & 3) + (e & 1))) hidden |= 1u << (4 * n + e);
+        }
+    }
+    float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        z[n][e] = hidden >> (4 * n + e) & 1 ? -INFINITY : z[n][e] * a.c;
+        if (e < 2) x0 = fmaxf(x0, z[n][e]);
+        else x1 = fmaxf(x1, z[n][e]);
+      }
+#pragma unroll
+    for (int w = 1; w < 4; w <<= 1) {
+      x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, w));
+      x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, w));
+    }
+    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+    const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
+    const float f0 = ex2(m0 - b0), f1 = ex2(m1 - b1);
+    if (__any_sync(0xffffffffu, n0 != m0 || n1 != m1)) {
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) o[i][0] *= f0, o[i][1] *= f0, o[i][2] *= f1, o[i][3] *= f1;
+      l0 *= f0, l1 *= f1;
+      m0 = n0, m1 = n1;
+    }
+    uint32_t hi[4], lo[4];                             // A fragment: n = 0: keys 0..7, n = 1: keys 8..15
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const float base = e ? b1 : b0, u = ex2(z[n][e] - base), w = ex2(z[n][e + 1] - base);
+        (e ? l1 : l0) += u + w;
+        z[n][e] = u, z[n][e + 1] = w;
+        const uint32_t x = pack_bf16x2(u, w);
+        hi[2 * n + e / 2] = x;
+        lo[2 * n + e / 2] = pack_bf16x2(u - bf16_lo_f32(x), w - bf16_hi_f32(x));
+      }
+    // A product would take an infinity or NaN of a hidden key's value into the row (0 * inf): where one of
+    // the tile's new rows has such a value, the sums skip hidden keys one by one.
+    bool odd = false;
+    if (edge && __any_sync(0xffffffffu, hidden)) {
+      const int first = max(q.cached - key0, 0), n = (min(keys.hi - key0, 16) - first) * kC;
+      for (int i = lane; i < n; i += 32) {
+        const uint4 v = *reinterpret_cast<const uint4*>(s_smem + t % L::kStages * L::kStage + L::kHalf +
+                                                        (16 * warp + first + i / kC) * (D * 2) + (i % kC << 4));
+        odd |= !(bf16x2_finite(v.x) && bf16x2_finite(v.y) && bf16x2_finite(v.z) && bf16x2_finite(v.w));
+      }
+      odd = __any_sync(0xffffffffu, odd);
+    }
+    if (!odd) {
+      const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      const int row = 16 * warp + (lane & 15);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t b[4];
+        ldsm4t(b, vs + row * (D * 2) + (((2 * i + (lane >> 4)) ^ (row & 7)) << 4));
+        mma_bf16_16816(o[2 * i], ph, b[0], b[1]);
+        mma_bf16_16816(o[2 * i], pl, b[0], b[1]);
+        mma_bf16_16816(o[2 * i + 1], ph, b[2], b[3]);
+        mma_bf16_16816(o[2 * i + 1], pl, b[2], b[3]);
+      }
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < 16; ++j) {
+        const int from = (lane & 28) | (j & 7) >> 1, row = 16 * warp + j;
+        float pa = 0.f, pb = 0.f;
+        bool ha = false, hb = false;
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float u = __shfl_sync(0xffffffffu, z[n][e], from), w = __shfl_sync(0xffffffffu, z[n][e + 2], from);
+            const unsigned hd = __shfl_sync(0xffffffffu, hidden, from) >> (4 * n + e);
+            if (j == 8 * n + 2 * (from & 3) + e) pa = u, pb = w, ha = hd & 1, hb = hd & 4;
+          }
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const uint32_t v = *reinterpret_cast<const uint32_t*>(s_smem + t % L::kStages * L::kStage + L::kHalf + row * (D * 2) +
+                                                                ((i ^ (row & 7)) << 4) + 4 * (lane & 3));
+          if (!ha) o[i][0] = fmaf(pa, bf16_lo_f32(v), o[i][0]), o[i][1] = fmaf(pa, bf16_hi_f32(v), o[i][1]);
+          if (!hb) o[i][2] = fmaf(pb, bf16_lo_f32(v), o[i][2]), o[i][3] = fmaf(pb, bf16_hi_f32(v), o[i][3]);
+        }
+      }
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  // the four warps' parts, then their sum over the first one's place
+  float* os = reinterpret_cast<float*>(s_smem);
+#pragma unroll
+  for (int w = 1; w < 4; w <<= 1) {
+    l0 += __shfl_xor_sync(0xffffffffu, l0, w);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, w);
+  }
+  if ((lane & 3) == 0) sm_m[warp][r0] = m0, sm_m[warp][r1] = m1, sm_l[warp][r0] = l0, sm_l[warp][r1] = l1;
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    const int d = 8 * i + 2 * (lane & 3);
+    if (r0 < vecs) *reinterpret_cast<float2*>(os + (warp * kSVecs + r0) * L::kPitch + d) = make_float2(o[i][0], o[i][1]);
+    if (r1 < vecs) *reinterpret_cast<float2*>(os + (warp * kSVecs + r1) * L::kPitch + d) = make_float2(o[i][2], o[i][3]);
+  }
+  __syncthreads();
+  const long long pair = (long long)s * a.kv.n_kv_heads + h;
+  for (int t = threadIdx.x; t < vecs * (D / 4); t += kSThreads) {
+    const int r = t / (D / 4), d = t % (D / 4) * 4;
+    float mx = -INFINITY, sum = 0.f;
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm_m[w][r]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2f(sm_m[w][r] - base);
+      const float4 y = *reinterpret_cast<const float4*>(os + (w * kSVecs + r) * L::kPitch + d);
+      sum = fmaf(f, sm_l[w][r], sum);
+      x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
+    }
+    if (a.splits == 1) {
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      store4(out_at<uint16_t, D>(a, q, h, r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+    } else if (a.part) {
+      float* to = a.part + ((pair * a.splits + split) * kSVecs + r) * (D + 4);
+      *reinterpret_cast<float4*>(to + d) = x;
+      if (d == 0) to[D] = mx, to[D + 1] = sum;
+    } else {
+      *reinterpret_cast<float4*>(os + r * L::kPitch + d) = x;       // (this thread alone read these places)
+      if (d == 0) fin_m[r] = mx, fin_l[r] = sum;
+    }
+  }
+  if (a.splits > 1 && !a.part) join_cluster<uint16_t, D>(a, q, h, 0, vecs, os, L::kPitch, fin_m, fin_l);
+}
+
+// Joins parts in the workspace: a CTA per (KV head, sequence), a thread per four elements of o.
+template <int D>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
+  const int h = blockIdx.x, s = blockIdx.y;
+  tc::pdl_wait();
+  tc::pdl_trigger();
+  const Seq q = load_seq(a.ch, s);
+  if (q.n <= 0 || q.n > kSVecs / a.group) return;
+  const int vecs = q.n * a.group;
+  const long long pair = (long long)s * a.kv.n_kv_heads + h;
+  for (int t = threadIdx.x; t < vecs * (D / 4); t += 256) {
+    const int r = t / (D / 4), d = t % (D / 4) * 4;
+    const float* from = a.part + (pair * a.splits * kSVecs + r) * (D + 4);
+    constexpr long long kStep = kSVecs * (D + 4);
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll 8
+    for (int z = 0; z < a.splits; ++z) mx = fmaxf(mx, __ldcg(from + z * kStep + D));
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int z = 0; z < a.splits; ++z) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(from + z * kStep + D));
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(from + z * kStep + d));
+      const float f = exp2f(ml.x - base);
+      sum = fmaf(f, ml.y, sum);
+      x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    store4(out_at<uint16_t, D>(a, q, h, r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+  }
+}
+
+// Launch with clusters of `cluster` CTAs along x.
+template <class K>
+cudaError_t launch_clusters(K* kernel, dim3 grid, int threads, int cluster, size_t smem, cudaStream_t st, const AttnArgs& a) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 // The shared-memory opt-in is a property of the function: set once per device.
@@ -217,19 +613,56 @@ cudaError_t opt_in(K* kernel, int bytes, std::atomic<unsigned>& done) {
   return e;
 }
 
+// Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for two CTAs per SM,
+// each with at least `least` keys, at most `most` parts (a power of two).
+int splits_for(long long work, int max_tokens, int least, int most) {
+  const int n_sm = sm_count();
+  int z = 1;
+  while (z < most && work * z < 2 * n_sm && max_tokens / (2 * z) >= least) z *= 2;
+  return z;
+}
+
 template <class T, int D, int RM>
-cudaError_t launch_f32(const AttnArgs& a, cudaStream_t st) {
+cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
   const int bytes = (int)sizeof(FSmem<D, RM>);
   cudaError_t e = opt_in(attn_f32_kernel<T, D, RM>, bytes, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)a.ch.max_rows * a.group + 16 * RM - 1) / (16 * RM);
-  return tc::launch(true, attn_f32_kernel<T, D, RM>, dim3((unsigned)tiles, a.kv.n_kv_heads, a.ch.n_seqs), dim3(kFThreads), bytes,
-                    st, a);
+  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8);
+  return launch_clusters(attn_f32_kernel<T, D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
+                         a.splits, bytes, st, a);
 }
 template <class T, int D>
 cudaError_t launch_f32(const AttnArgs& a, cudaStream_t st) {
   return (long long)a.ch.max_rows * a.group <= 16 ? launch_f32<T, D, 1>(a, st) : launch_f32<T, D, 4>(a, st);
+}
+
+struct StepPlan {
+  int splits;
+  bool in_workspace;
+};
+// Up to 8 parts are joined by the CTAs of a cluster; where that leaves most SMs idle and the
+// keys are many, more parts go through the workspace.
+StepPlan plan_step(const mcd_paged_kv& kv, const mcd_chunks& ch) {
+  const long long pairs = (long long)kv.n_kv_heads * ch.n_seqs;
+  const int z = splits_for(pairs, ch.max_tokens, 64, 8);
+  const int more = splits_for(pairs, ch.max_tokens, 512, 128);
+  return more > 8 ? StepPlan{more, true} : StepPlan{z, false};
+}
+
+template <int D>
+cudaError_t launch_step(AttnArgs a, void* workspace, cudaStream_t st) {
+  static std::atomic<unsigned> done{0};
+  const int bytes = SLayout<D>::kBytes;
+  cudaError_t e = opt_in(attn_step_kernel<D>, bytes, done);
+  if (e != cudaSuccess) return e;
+  const StepPlan p = plan_step(a.kv, a.ch);
+  a.splits = p.splits;
+  a.part = p.in_workspace ? static_cast<float*>(workspace) : nullptr;
+  e = launch_clusters(attn_step_kernel<D>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a);
+  if (e == cudaSuccess && a.part) e = tc::launch(true, attn_join_kernel<D>, dim3(a.kv.n_kv_heads, a.ch.n_seqs), dim3(256), 0, st, a);
+  return e;
 }
 
 }  // namespace
@@ -239,8 +672,11 @@ cudaError_t launch_f32(const AttnArgs& a, cudaStream_t st) {
 using namespace mcd;
 
 extern "C" int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads) {
-  (void)kv, (void)chunks, (void)n_q_heads;
-  return 0;
+  using namespace paged;
+  if (check_kv(kv) != MCD_OK || check_chunks(chunks, kv) != MCD_OK || no_rows(chunks) || n_q_heads <= 0) return 0;
+  if (kv->dtype != MCD_WEIGHT_BF16) return 0;
+  const StepPlan p = plan_step(*kv, *chunks);
+  return p.in_workspace ? 4ll * kv->n_kv_heads * chunks->n_seqs * p.splits * kSVecs * (kv->head_dim + 4) : 0;
 }
 
 extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks,
@@ -264,10 +700,12 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
     return MCD_ERR_UNSUPPORTED;
   const int64_t need = mcd_paged_attention_workspace(kv, chunks, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
-  const AttnArgs a{*kv, *chunks, q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words,
+  const AttnArgs a{*kv, *chunks, q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, nullptr,
                    scale * 1.4426950408889634f};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
     return cuda_status(kv->head_dim == 64 ? launch_f32<float, 64>(a, st) : launch_f32<float, 128>(a, st));
+  if ((int64_t)chunks->max_rows * a.group <= kSVecs)
+    return cuda_status(kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st));
   return cuda_status(kv->head_dim == 64 ? launch_f32<uint16_t, 64>(a, st) : launch_f32<uint16_t, 128>(a, st));
 }
