@@ -1,123 +1,12 @@
-// mcd_paged_attention (include/mcd_cache.h).
-//
-// The mathematics, per query vector q of a row (keys j over the visible positions):
-//   s_j = scale q . k_j,  m = max s_j,  l = sum e^(s_j - m),  o = sum e^(s_j - m) v_j / l
-// in one pass over the keys with a running m, l and unnormalised o (rescaled by e^(m_old - m_new) when
-// m grows); in base 2: e^(s - m) = 2^(c q.k - c max q.k), c = scale log2(e).  Parts of the keys are
-// joined by the same rule.
-//
-// The query vectors of one KV head (its group of query heads x the sequence's new rows, "packed"
-// vector p = row * group + head of the group) read the same keys, so a CTA takes a tile of packed vectors
-// of one (sequence, KV head).
-#include <cooperative_groups.h>
-
+// mcd_paged_attention (include/mcd_cache.h): fp32 caches, and bf16 ones with up to 16 query vectors of a
+// KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
 #include <algorithm>
 
-#include "mcd_cache.cuh"
+#include "mcd_attn.cuh"
 
 namespace mcd {
 namespace paged {
 namespace {
-
-struct AttnArgs {
-  mcd_paged_kv kv;
-  mcd_chunks ch;
-  const void* q;
-  void* out;
-  const uint32_t* mask;
-  int* err;
-  long long q_stride, out_stride;
-  int layer, group, mask_words;
-  int splits;              // parts of a sequence's keys
-  float* part;             // workspace of the parts (null: the CTAs of a cluster join them)
-  float c;                 // scale * log2(e)
-};
-
-// Whether packed vectors of row i (of the sequence's new rows) see key `pos`; keys below q.cached are seen by all.
-__device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int pos) {
-  const int j = pos - q.cached;
-  if (j < 0) return true;
-  if (j >= q.n || i >= q.n) return false;
-  if (!a.mask) return j <= i;
-  return (__ldg(a.mask + (long long)(q.row0 + i) * a.mask_words + (j >> 5)) >> (j & 31)) & 1u;
-}
-
-// Place (elements) of position pos of KV head h in the layer's pages; -1 for a page outside the pool.
-__device__ __forceinline__ long long key_at(const AttnArgs& a, int s, int h, int pos) {
-  const int page = __ldg(a.ch.table + (long long)s * a.ch.table_stride + pos / a.kv.page_size);
-  if (page < 0 || page >= a.kv.n_pages) {
-    report(a.err, MCD_ERR_INVALID_ARG);
-    return -1;
-  }
-  return a.layer * a.kv.layer_stride + page * a.kv.page_stride + h * a.kv.head_stride +
-         pos % a.kv.page_size * a.kv.token_stride;
-}
-
-// 2^x by the hardware's approximation (relative error 2^-22).
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-template <class T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
-template <>
-__device__ __forceinline__ float4 load4<uint16_t>(const uint16_t* p) {
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(p));
-  return make_float4(bf16_lo_f32(w.x), bf16_hi_f32(w.x), bf16_lo_f32(w.y), bf16_hi_f32(w.y));
-}
-__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(uint16_t* p, float4 v) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-}
-
-// Output element of packed vector p, dimension d.
-template <class T, int D>
-__device__ __forceinline__ T* out_at(const AttnArgs& a, const Seq& q, int h, long long p, int d) {
-  return static_cast<T*>(a.out) + (q.row0 + p / a.group) * a.out_stride + (h * a.group + p % a.group) * D + d;
-}
-
-// Part z of the keys [0, n_keys), in whole tiles of `tile` keys.
-struct Span {
-  int lo, hi;
-};
-__device__ __forceinline__ Span part_of(int n_keys, int z, int splits, int tile) {
-  const int per = ((n_keys + splits - 1) / splits + tile - 1) / tile * tile;
-  const long long lo = min((long long)z * per, (long long)n_keys);
-  return {(int)lo, (int)min((long long)n_keys, lo + per)};
-}
-
-// Joins the parts of `vecs` packed vectors (from p0 on) that the CTAs of a cluster hold in the same places of their shared
-// memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
-// m = -inf and l = 0; nothing at all gives zeros.
-template <class T, int D>
-__device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, long long p0, int vecs, float* o, int pitch,
-                                             float* m, float* l) {
-  namespace cg = cooperative_groups;
-  cg::cluster_group cl = cg::this_cluster();
-  cl.sync();
-  const int n = (int)cl.num_blocks(), threads = (int)blockDim.x;
-  for (int t = (int)cl.block_rank() * threads + threadIdx.x; t < vecs * (D / 4); t += n * threads) {
-    const int r = t / (D / 4), d = t % (D / 4) * 4;
-    float mx = -INFINITY;
-    for (int z = 0; z < n; ++z) mx = fmaxf(mx, *cl.map_shared_rank(m + r, z));
-    const float base = mx == -INFINITY ? 0.f : mx;
-    float sum = 0.f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int z = 0; z < n; ++z) {
-      const float w = exp2f(*cl.map_shared_rank(m + r, z) - base);
-      const float4 y = *reinterpret_cast<const float4*>(cl.map_shared_rank(o + r * pitch + d, z));
-      sum = fmaf(w, *cl.map_shared_rank(l + r, z), sum);
-      x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
-    }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    store4(out_at<T, D>(a, q, h, p0 + r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
-  }
-  cl.sync();                                           // nobody leaves while others read
-}
 
 // ---- plain fp32 arithmetic -------------------------------------------------------------------------
 // A CTA of 16 x 16 threads takes 16 RM packed vectors against tiles of 64 keys: thread (ty, tx) has rows
@@ -131,7 +20,7 @@ struct FSmem {
   float q[16 * RM][D + 4], k[kFN][D + 4], v[kFN][D], p[16 * RM][kFN + 4], m[16 * RM], l[16 * RM];
 };
 
-template <class T, int D, int RM>
+template <int D, int RM>
 __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
   extern __shared__ __align__(16) uint8_t f_smem[];
   FSmem<D, RM>& sm = *reinterpret_cast<FSmem<D, RM>*>(f_smem);
@@ -153,7 +42,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
     const long long p = p0 + r;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p < vecs)
-      x = load4(static_cast<const T*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + d);
+      x = load4(static_cast<const float*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + d);
     *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
   }
   float m[RM], l[RM];
@@ -173,8 +62,8 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       if (k0 + r < keys.hi) {
         const long long at = key_at(a, s, h, k0 + r);
         if (at >= 0) {
-          x = load4(static_cast<const T*>(a.kv.k) + at + d);
-          y = load4(static_cast<const T*>(a.kv.v) + at + d);
+          x = load4(static_cast<const float*>(a.kv.k) + at + d);
+          y = load4(static_cast<const float*>(a.kv.v) + at + d);
         }
       }
       *reinterpret_cast<float4*>(&sm.k[r][d]) = x;
@@ -261,7 +150,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       for (int c = 0; c < kDC; ++c) *reinterpret_cast<float4*>(&os[ty * RM + r][tx * 4 + 64 * c]) = o[r][c];
       if (tx == 0) sm.m[ty * RM + r] = m[r], sm.l[ty * RM + r] = l[r];
     }
-    join_cluster<T, D>(a, q, h, p0, (int)min((long long)kBM, vecs - p0), &os[0][0], D + 4, sm.m, sm.l);
+    join_cluster<float, D>(a, q, h, p0, (int)min((long long)kBM, vecs - p0), &os[0][0], D + 4, sm.m, sm.l);
     return;
   }
 #pragma unroll
@@ -271,7 +160,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
     const float f = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
     for (int c = 0; c < kDC; ++c)
-      store4(out_at<T, D>(a, q, h, p, tx * 4 + 64 * c), make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
+      store4(out_at<float, D>(a, q, h, p, tx * 4 + 64 * c), make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
   }
 }
 
@@ -302,10 +191,6 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-__device__ __forceinline__ bool bf16x2_finite(uint32_t w) {
-  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
-}
-
 template <int D>
 __global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) {
   using L = SLayout<D>;
@@ -581,38 +466,6 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
   }
 }
 
-// Launch with clusters of `cluster` CTAs along x.
-template <class K>
-cudaError_t launch_clusters(K* kernel, dim3 grid, int threads, int cluster, size_t smem, cudaStream_t st, const AttnArgs& a) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster;
-  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
-}
-
-// The shared-memory opt-in is a property of the function: set once per device.
-template <class K>
-cudaError_t opt_in(K* kernel, int bytes, std::atomic<unsigned>& done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const unsigned bit = 1u << (dev & 31);
-  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
-  return e;
-}
-
 // Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for two CTAs per SM,
 // each with at least `least` keys, at most `most` parts (a power of two).
 int splits_for(long long work, int max_tokens, int least, int most) {
@@ -622,20 +475,20 @@ int splits_for(long long work, int max_tokens, int least, int most) {
   return z;
 }
 
-template <class T, int D, int RM>
+template <int D, int RM>
 cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
   const int bytes = (int)sizeof(FSmem<D, RM>);
-  cudaError_t e = opt_in(attn_f32_kernel<T, D, RM>, bytes, done);
+  cudaError_t e = opt_in(attn_f32_kernel<D, RM>, bytes, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)a.ch.max_rows * a.group + 16 * RM - 1) / (16 * RM);
   a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8);
-  return launch_clusters(attn_f32_kernel<T, D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
+  return launch_clusters(attn_f32_kernel<D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
                          a.splits, bytes, st, a);
 }
-template <class T, int D>
+template <int D>
 cudaError_t launch_f32(const AttnArgs& a, cudaStream_t st) {
-  return (long long)a.ch.max_rows * a.group <= 16 ? launch_f32<T, D, 1>(a, st) : launch_f32<T, D, 4>(a, st);
+  return (long long)a.ch.max_rows * a.group <= 16 ? launch_f32<D, 1>(a, st) : launch_f32<D, 4>(a, st);
 }
 
 struct StepPlan {
@@ -700,12 +553,21 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
     return MCD_ERR_UNSUPPORTED;
   const int64_t need = mcd_paged_attention_workspace(kv, chunks, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
-  const AttnArgs a{*kv, *chunks, q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, nullptr,
+  const AttnArgs a{*kv, *chunks, q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, 0, nullptr,
                    scale * 1.4426950408889634f};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
-    return cuda_status(kv->head_dim == 64 ? launch_f32<float, 64>(a, st) : launch_f32<float, 128>(a, st));
-  if ((int64_t)chunks->max_rows * a.group <= kSVecs)
-    return cuda_status(kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st));
-  return cuda_status(kv->head_dim == 64 ? launch_f32<uint16_t, 64>(a, st) : launch_f32<uint16_t, 128>(a, st));
+    return cuda_status(kv->head_dim == 64 ? launch_f32<64>(a, st) : launch_f32<128>(a, st));
+  // bf16: sequences of up to 16 vectors per KV head go to the step kernel, longer ones to the chunk kernel;
+  // the bounds tell when there are only the ones or the others
+  AttnArgs b = a;
+  cudaError_t e = cudaSuccess;
+  const bool chunks_too = (int64_t)chunks->max_rows * a.group > kSVecs;
+  const bool steps_too = !chunks_too || (int64_t)chunks->n_rows < (int64_t)chunks->n_seqs * chunks->max_rows;
+  if (steps_too) e = kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st);
+  if (e == cudaSuccess && chunks_too) {
+    b.least_vecs = steps_too ? kSVecs : 0;
+    e = launch_chunk(b, st);
+  }
+  return cuda_status(e);
 }

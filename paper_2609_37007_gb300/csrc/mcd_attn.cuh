@@ -1,0 +1,161 @@
+// Shared by the kernels of mcd_paged_attention.
+//
+// The mathematics, per query vector q of a row (keys j over the visible positions):
+//   s_j = scale q . k_j,  m = max s_j,  l = sum e^(s_j - m),  o = sum e^(s_j - m) v_j / l
+// in one pass over the keys with a running m, l and unnormalised o (rescaled by e^(m_old - m_new) when
+// m grows); in base 2: e^(s - m) = 2^(c q.k - max c q.k), c = scale log2(e).  Parts of the keys are
+// joined by the same rule.
+//
+// The query vectors of one KV head (its group of query heads x the sequence's new rows, "packed"
+// vector p = row * group + head of the group) read the same keys, so a CTA takes a tile of packed vectors
+// of one (sequence, KV head).
+#pragma once
+#include <cooperative_groups.h>
+
+#include "mcd_cache.cuh"
+
+namespace mcd {
+namespace paged {
+
+struct AttnArgs {
+  mcd_paged_kv kv;
+  mcd_chunks ch;
+  const void* q;
+  void* out;
+  const uint32_t* mask;
+  int* err;
+  long long q_stride, out_stride;
+  int layer, group, mask_words;
+  int splits;              // parts of a sequence's keys
+  int least_vecs;          // the chunk kernel takes sequences with more packed vectors than this
+  float* part;             // workspace of the parts (null: the CTAs of a cluster join them)
+  float c;                 // scale * log2(e)
+};
+
+// Whether packed vectors of row i (of the sequence's new rows) see key `pos`; keys below q.cached are seen by all.
+__device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int pos) {
+  const int j = pos - q.cached;
+  if (j < 0) return true;
+  if (j >= q.n || i >= q.n) return false;
+  if (!a.mask) return j <= i;
+  return (__ldg(a.mask + (long long)(q.row0 + i) * a.mask_words + (j >> 5)) >> (j & 31)) & 1u;
+}
+
+// Place (elements) of position pos of KV head h in the layer's pages; -1 for a page outside the pool.
+__device__ __forceinline__ long long key_at(const AttnArgs& a, int s, int h, int pos) {
+  const int page = __ldg(a.ch.table + (long long)s * a.ch.table_stride + pos / a.kv.page_size);
+  if (page < 0 || page >= a.kv.n_pages) {
+    report(a.err, MCD_ERR_INVALID_ARG);
+    return -1;
+  }
+  return a.layer * a.kv.layer_stride + page * a.kv.page_stride + h * a.kv.head_stride +
+         pos % a.kv.page_size * a.kv.token_stride;
+}
+
+// 2^x by the hardware's approximation (relative error 2^-22).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <class T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) { return __ldg(reinterpret_cast<const float4*>(p)); }
+template <>
+__device__ __forceinline__ float4 load4<uint16_t>(const uint16_t* p) {
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>(p));
+  return make_float4(bf16_lo_f32(w.x), bf16_hi_f32(w.x), bf16_lo_f32(w.y), bf16_hi_f32(w.y));
+}
+__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(uint16_t* p, float4 v) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+}
+
+// Output element of packed vector p, dimension d.
+template <class T, int D>
+__device__ __forceinline__ T* out_at(const AttnArgs& a, const Seq& q, int h, long long p, int d) {
+  return static_cast<T*>(a.out) + (q.row0 + p / a.group) * a.out_stride + (h * a.group + p % a.group) * D + d;
+}
+
+// Part z of the keys [0, n_keys), in whole tiles of `tile` keys.
+struct Span {
+  int lo, hi;
+};
+__device__ __forceinline__ Span part_of(int n_keys, int z, int splits, int tile) {
+  const int per = ((n_keys + splits - 1) / splits + tile - 1) / tile * tile;
+  const long long lo = min((long long)z * per, (long long)n_keys);
+  return {(int)lo, (int)min((long long)n_keys, lo + per)};
+}
+
+// Joins the parts of `vecs` packed vectors (from p0 on) that the CTAs of a cluster hold in the same places of their shared
+// memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
+// m = -inf and l = 0; nothing at all gives zeros.
+template <class T, int D>
+__device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, long long p0, int vecs, float* o, int pitch,
+                                             float* m, float* l) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cl = cg::this_cluster();
+  cl.sync();
+  const int n = (int)cl.num_blocks(), threads = (int)blockDim.x;
+  for (int t = (int)cl.block_rank() * threads + threadIdx.x; t < vecs * (D / 4); t += n * threads) {
+    const int r = t / (D / 4), d = t % (D / 4) * 4;
+    float mx = -INFINITY;
+    for (int z = 0; z < n; ++z) mx = fmaxf(mx, *cl.map_shared_rank(m + r, z));
+    const float base = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z = 0; z < n; ++z) {
+      const float w = exp2f(*cl.map_shared_rank(m + r, z) - base);
+      const float4 y = *reinterpret_cast<const float4*>(cl.map_shared_rank(o + r * pitch + d, z));
+      sum = fmaf(w, *cl.map_shared_rank(l + r, z), sum);
+      x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    store4(out_at<T, D>(a, q, h, p0 + r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+  }
+  cl.sync();                                           // nobody leaves while others read
+}
+
+__device__ __forceinline__ bool bf16x2_finite(uint32_t w) {
+  return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
+}
+
+// Launch with clusters of `cluster` CTAs along x.
+template <class K, class... Args>
+cudaError_t launch_clusters(K* kernel, dim3 grid, int threads, int cluster, size_t smem, cudaStream_t st, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// The shared-memory opt-in is a property of the function: set once per device.
+template <class K>
+cudaError_t opt_in(K* kernel, int bytes, std::atomic<unsigned>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned bit = 1u << (dev & 31);
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
+  return e;
+}
+
+// Sequences with more than a.least_vecs packed vectors, bf16 (mcd_attn_chunk.cu).
+cudaError_t launch_chunk(const AttnArgs& a, cudaStream_t st);
+
+}  // namespace paged
+}  // namespace mcd
