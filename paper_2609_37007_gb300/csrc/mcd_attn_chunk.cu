@@ -35,8 +35,8 @@ struct CLayout {
   static constexpr int kTileBytes = kCTile * D * 2;                     // one Q, K or V tile
   static constexpr int kStages = D == 128 ? 4 : 8;
   static constexpr int kRing = 2 * kTileBytes;
-  static constexpr int kBar = kRing + kStages * kTileBytes;             // full[S] empty[S] q s[2] p[2] o[2] drain v_full[S / 2] v_seen[S / 2]
-  static constexpr int kBars = 3 * kStages + 8;
+  static constexpr int kBar = kRing + kStages * kTileBytes;             // full[S] empty[S] q s[2] p[2][2] o[2] drain v_full[S / 2] v_seen[S / 2]
+  static constexpr int kBars = 3 * kStages + 10;
   static constexpr int kMisc = kBar + kBars * 8;                        // tensor memory address, abort, odd
   static constexpr int kStat = kMisc + 16;                              // m, l of the rows (parts)
   static constexpr int kBytes = kStat + 2 * kCRows * 4 + 1024;          // + alignment
@@ -87,12 +87,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
 __device__ __forceinline__ void tmem_loaded(uint32_t (&r)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : MCD_P8(r, 0), MCD_P8(r, 8), MCD_P8(r, 16), MCD_P8(r, 24) : : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-      "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::MCD_I8(r, 0), MCD_I8(r, 8), MCD_I8(r, 16), MCD_I8(r, 24), "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::MCD_I8(r, 0),
@@ -100,6 +94,61 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// One lane of the warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+  return p != 0;
+}
+
+// A warp's bounded wait (the same answer in every lane).  The test alone where the phase is over: a look at the abort
+// flag beside it doubled the 64 cycles that it takes, six times a pair of tiles in the warp that issues.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* abort_flag) {
+  constexpr unsigned long long kWait = 2000000000ull;
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const uint64_t t0 = globaltimer();
+  for (int n = 1;; ++n) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (n % 16) continue;
+    const bool given_up = *abort_flag != 0, late = globaltimer() - t0 > kWait;
+    if (__any_sync(0xffffffffu, given_up || late)) {
+      if ((threadIdx.x & 31) == 0) {
+        if (!given_up) report(err, MCD_ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+      return false;
+    }
+  }
+}
+
+// Two fp32 operations an instruction.
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+  return d;
+}
+__device__ __forceinline__ void unpack2(uint64_t d, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(d)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 
 // Bits of the positions pos0 .. pos0 + 31 that row i sees.
 __device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, int i, int pos0) {
@@ -153,7 +202,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
   extern __shared__ uint8_t c_smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(c_smem_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBar);
-  uint64_t *empty = full + S, *q_full = empty + S, *s_full = q_full + 1, *p_full = s_full + 2, *o_full = p_full + 2,
+  uint64_t *empty = full + S, *q_full = empty + S, *s_full = q_full + 1, *p_full = s_full + 2, *o_full = p_full + 4,
            *drain = o_full + 2, *v_full = drain + 1, *v_seen = v_full + S / 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kMisc);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMisc + 4);
@@ -198,16 +247,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
       mbar_init(&empty[i], 1);
     }
     mbar_init(q_full, 8);
+    mbar_init(drain, 1);
     for (int w = 0; w < 2; ++w) {
       mbar_init(&s_full[w], 1);
-      mbar_init(&p_full[w], 4);
+      mbar_init(&p_full[2 * w], 4);                    // either half of P
+      mbar_init(&p_full[2 * w + 1], 4);
       mbar_init(&o_full[w], 1);
     }
     for (int i = 0; i < S / 2; ++i) {
       mbar_init(&v_full[i], 1);
       mbar_init(&v_seen[i], 1);
     }
-    mbar_init(drain, 1);
     *abort_flag = 0;
     *odd = 0;
     fence_barrier_init();
@@ -263,72 +313,66 @@ __global__ void __launch_bounds__(kCThreads, 1)
     if (lane == 0)
       for (uint32_t n = i > (uint32_t)S ? i - S : 0u; n < i; ++n) tc::tc_wait(load_bar(n), load_phase(n), a.err, kWait);
   } else if (warp == 9) {
-    if (lane == 0) {
-      // ---- products
-      constexpr uint32_t kQk = tc::idesc_bf16_n(kCTile), kPv = tc::idesc_bf16_n(D) | 1u << 16;     // (bit 16: B is n-major)
-      bool ok = true;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok && (!tc::tc_wait(bar, parity, a.err, kWait) || *abort_flag)) {
-          *abort_flag = 1;
-          ok = false;
-        }
-        return ok;
-      };
-      auto qk = [&](int w, int j) {
-        const uint32_t qa = smem_u32(smem + w * L::kTileBytes), kb = smem_u32(stage(2 * j));
+    // ---- products.  The whole warp runs the loop, so that descriptors stay in uniform registers, and one elected
+    // lane (always the same) issues: from a branch of lane 0 alone an issue took 130 cycles, twice what the
+    // product does.  One warp for both tiles: with one each, the products of the two mixed and each waited for both
+    // (460 against 533 us for 11,559 rows over up to 8,500 keys).
+    constexpr uint32_t kQk = tc::idesc_bf16_n(kCTile), kPv = tc::idesc_bf16_n(D) | 1u << 16;       // (bit 16: B is n-major)
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && warp_wait(bar, parity, a.err, abort_flag);
+      return ok;
+    };
+    auto wait_load = [&](uint32_t i) { return wait(load_bar(i), load_phase(i)); };
+    auto qk = [&](int w, int j) {
+      const uint32_t qa = smem_u32(smem + w * L::kTileBytes), kb = smem_u32(stage(2 * j));
+      if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
           const uint32_t at = (k >> 2) * kChunk + (k & 3) * 32;
           tc::umma_bf16(s_col(w), tc::sw128_desc(qa + at), tc::sw128_desc(kb + at), kQk, k > 0);
         }
         tc::umma_commit(&s_full[w]);
-      };
-      auto pv = [&](int w, int j) {
-        const uint32_t vb = smem_u32(stage(2 * j + 1));
+      }
+    };
+    auto pv = [&](int w, int j) {
+      const uint32_t vb = smem_u32(stage(2 * j + 1));
 #pragma unroll
-        for (int k = 0; k < kCTile / 16; ++k)
-          umma_ts(o_col(w), s_col(w) + 8 * k, v_desc(vb + k * 2048, kChunk), kPv, (j | k) != 0);
-        if (j + 1 == (w ? n_b : n_a)) tc::umma_commit(&o_full[w]);
-      };
-      auto wait_load = [&](uint32_t i) { return wait(load_bar(i), load_phase(i)); };
-      if (n_tiles > 0 && wait(q_full, 0) && wait_load(0)) {
+      for (int half = 0; half < 2; ++half) {
+        if (!wait(&p_full[2 * w + half], j & 1)) return;
         tc::tc_fence_after();
-        if (n_a > 0) qk(0, 0);
-        if (n_b > 0) qk(1, 0);
-        tc::umma_commit(&empty[0]);
-        for (int j = 0; j < n_tiles && ok; ++j) {
-          if (!wait_load(2 * j + 1)) break;
-          if (const int n = j - first_look; n >= 0 && !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) break;
-          if (j < n_a) {
-            if (!wait(&p_full[0], j & 1)) break;
-            tc::tc_fence_after();
-            pv(0, j);
-          }
-          if (j + 1 < n_tiles && !wait_load(2 * j + 2)) break;
-          if (j + 1 < n_a) qk(0, j + 1);
-          if (j < n_b) {
-            if (!wait(&p_full[1], j & 1)) break;
-            tc::tc_fence_after();
-            pv(1, j);
-          }
-          tc::umma_commit(&empty[(2 * j + 1) % S]);
-          if (j + 1 < n_b) qk(1, j + 1);
-          if (j + 1 < n_tiles) tc::umma_commit(&empty[(2 * j + 2) % S]);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 4 * half; k < 4 * half + 4; ++k)
+            umma_ts(o_col(w), s_col(w) + 8 * k, v_desc(vb + k * 2048, kChunk), kPv, (j | k) != 0);
         }
       }
-      tc::umma_commit(drain);
-      tc::tc_wait(drain, 0, a.err, kWait);
+      if (j + 1 == (w ? n_b : n_a) && elect_one()) tc::umma_commit(&o_full[w]);
+    };
+    if (n_tiles > 0 && wait(q_full, 0) && wait_load(0)) {
+      tc::tc_fence_after();
+      if (n_a > 0) qk(0, 0);
+      if (n_b > 0) qk(1, 0);
+      for (int j = 0; j < n_tiles; ++j) {
+        if (j + 1 < n_tiles && !wait_load(2 * j + 2)) break;
+        if (!wait_load(2 * j + 1)) break;
+        if (const int n = j - first_look; n >= 0 && !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) break;
+        if (j < n_a) pv(0, j);
+        if (!ok) break;
+        if (j + 1 < n_a) qk(0, j + 1);
+        if (j < n_b) pv(1, j);
+        if (!ok) break;
+        if (j + 1 < n_b) qk(1, j + 1);
+      }
     }
+    if (elect_one()) tc::umma_commit(drain);
+    tc::tc_wait(drain, 0, a.err, kWait);
     __syncwarp();
   } else if (warp == 10) {
     // ---- V tiles that are seen in part
     for (int j = first_look; j < n_tiles; ++j) {
       const uint32_t i = 2 * j + 1;
-      const bool ok = tc::tc_wait(load_bar(i), load_phase(i), a.err, kWait) && !*abort_flag;
-      if (!__all_sync(0xffffffffu, ok)) {
-        *abort_flag = 1;
-        break;
-      }
+      if (!warp_wait(load_bar(i), load_phase(i), a.err, abort_flag)) break;
       uint8_t* v = stage(i);
       const int k0 = keys.lo + j * kCTile, first = max(0, q.cached - k0), end = min(kCTile, keys.hi - k0);
       bool bad = false;
@@ -373,9 +417,13 @@ __global__ void __launch_bounds__(kCThreads, 1)
     float mc = 0.f;                                    // c * (the maximum in use)
     bool ok = true;
     for (int j = 0; j < n_mine; ++j) {
-      ok = tc::tc_wait(&s_full[w], j & 1, a.err, kWait) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
+      ok = warp_wait(&s_full[w], j & 1, a.err, abort_flag);
       if (!ok) break;
+      // S of the last tile j: every product before it is done, so K of tile j and V of tile j - 1 have been read
+      if (w == (n_b > 0) && t == 0) {
+        mbar_arrive(&empty[2 * j % S]);
+        if (j > 0) mbar_arrive(&empty[(2 * j - 1) % S]);
+      }
       tc::tc_fence_after();
       if (live) {
         uint32_t x[4][32];
@@ -397,9 +445,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
         float mx[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          mx[c] = __uint_as_float(x[c][0]);
+          mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
 #pragma unroll
-          for (int e = 1; e < 32; ++e) mx[c] = fmaxf(mx[c], __uint_as_float(x[c][e]));
+          for (int e = 2; e < 32; e += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1]));
         }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         // (m is -inf until the row has seen a key: then any is growth)
@@ -408,44 +456,59 @@ __global__ void __launch_bounds__(kCThreads, 1)
           const float n = fmaxf(m, top * a.c), base = n == -INFINITY ? 0.f : n, f = ex2(m - base);
           if (j > 0) {                                   // (S of tile j came after the product with P of tile j - 1)
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              uint32_t y[32];
-              tmem_ld32(o_col(w) + lanes + c, y);
-              tmem_loaded(y);
+            for (int c = 0; c < D; c += 16) {          // (few columns at a time: S fills the registers)
+              uint32_t y[16];
+              tc::tmem_ld16_async(o_col(w) + lanes + c, y);
+              tc::tmem_wait16(y);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-              tmem_st32(o_col(w) + lanes + c, y);
+              for (int e = 0; e < 16; e += 2) {
+                float u, v;
+                unpack2(mul2(pack2(__uint_as_float(y[e]), __uint_as_float(y[e + 1])), pack2(f, f)), u, v);
+                y[e] = __float_as_uint(u), y[e + 1] = __float_as_uint(v);
+              }
+              tmem_st16(o_col(w) + lanes + c, y);
             }
           }
           l *= f;
           m = n;
           mc = base;
         }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale = pack2(a.c, a.c), shift = pack2(-mc, -mc);
+        uint64_t sum[2] = {0ull, 0ull};                // (two zeros each)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t y[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float u = ex2(fmaf(__uint_as_float(x[c][2 * e]), a.c, -mc)), v = ex2(fmaf(__uint_as_float(x[c][2 * e + 1]), a.c, -mc));
-            sum[e & 3] += u + v;
+            float u, v;
+            unpack2(fma2(pack2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale, shift), u, v);
+            u = ex2(u), v = ex2(v);
+            sum[e & 1] = add2(sum[e & 1], pack2(u, v));
             y[e] = pack_bf16x2(u, v);
           }
           tmem_st16(s_col(w) + lanes + 16 * c, y);
+          if (c == 1) {                                // half of P: the product may start
+            tmem_stored();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[2 * w]);
+          }
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float u, v;
+        unpack2(add2(sum[0], sum[1]), u, v);
+        l += u + v;
         tmem_stored();
+      } else if (lane == 0) {
+        mbar_arrive(&p_full[2 * w]);
       }
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_full[w]);
+      if (lane == 0) mbar_arrive(&p_full[2 * w + 1]);
     }
     if (ok && n_mine > 0) {
-      ok = tc::tc_wait(&o_full[w], 0, a.err, kWait) && !*abort_flag;
-      ok = __all_sync(0xffffffffu, ok);
+      ok = warp_wait(&o_full[w], 0, a.err, abort_flag);
       tc::tc_fence_after();
     }
-    if (!ok) *abort_flag = 1;
     if (a.splits == 1 && ok && live) {
       if (__any_sync(0xffffffffu, *odd)) {
         for (int r = 0; r < 32; ++r) {
