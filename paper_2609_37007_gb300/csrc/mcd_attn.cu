@@ -165,24 +165,22 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
 }
 
 // ---- up to 16 packed vectors of a KV head, bf16 ------------------------------------------------------------
-// Reading K and V once is all there is to do (4 * 16 flop a byte at most), so the tile is built for loads:
-// four warps share tiles of 64 keys that travel through a ring of cp.async stages; warp w multiplies
-// its 16 keys with the 16 vectors on mma.m16n8k16 (scores: vectors x keys; o: vectors x dimensions) and
-// keeps a maximum, a sum and an o of its own, joined at the end.  Probabilities are multiplied as a hi + lo
-// pair of bf16 (16 bits): the second product costs nothing next to the loads.
-// Rows of a stage hold D bf16 in 16-byte chunks, chunk c at c ^ (row % 8): ldmatrix without conflicts.
+// Reading K and V once is all there is to do (4 * 16 flop a byte at most), so the kernel is built for loads: tiles of
+// 64 keys by TMA, a box per page and 64 dimensions, two or more tiles in flight per CTA and three CTAs on an SM.
+// Warp w multiplies its 16 keys of a tile with the 16 vectors on mma.m16n8k16 (scores: vectors x keys; o: vectors
+// x dimensions) and keeps a maximum, a sum and an o of its own, joined at the end.  Probabilities are multiplied as
+// a hi + lo pair of bf16 (16 bits): the second product costs nothing next to the loads.
+// (With cp.async copies of 16 bytes, 860 instructions a warp and tile, most of them addresses, bound it at half of
+// this rate.)
 constexpr int kSTile = 64, kSThreads = 128, kSVecs = 16;
 template <int D>
 struct SLayout {
-  static constexpr int kHalf = kSTile * D * 2, kStage = 2 * kHalf;      // K, then V
-  static constexpr int kStages = D == 128 ? 3 : 5;
-  static constexpr int kBytes = kStages * kStage;
+  static constexpr int kHalf = kSTile * D * 2, kStage = 2 * kHalf;      // K, then V: D / 64 chunks of 64 rows of 128 bytes
+  static constexpr int kStages = D == 128 ? 2 : 4;
+  static constexpr int kBytes = kStages * kStage + 1024;                // + alignment
   static constexpr int kPitch = D + 4;
-  static_assert(4 * kSVecs * kPitch * 4 <= kBytes, "the warps' o takes the stages' place");
+  static_assert(4 * kSVecs * kPitch * 4 <= kStages * kStage, "the warps' o takes the stages' place");
 };
-__device__ __forceinline__ void cpa16_or_zero(void* dst, const void* src, bool real) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -192,14 +190,23 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 template <int D>
-__global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kSThreads, 3)
+    attn_step_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using L = SLayout<D>;
-  constexpr int kC = D / 8;                            // chunks of a row
-  constexpr int kRows = kSThreads / kC;                // rows a pass of the copies takes: 8 or 16
-  extern __shared__ __align__(128) uint8_t s_smem[];
+  constexpr int S = L::kStages, kDC = D / 64, kChunk = kSTile * 128;
+  extern __shared__ uint8_t s_smem_raw[];
   __shared__ float sm_m[4][kSVecs], sm_l[4][kSVecs], fin_m[kSVecs], fin_l[kSVecs];
+  __shared__ uint64_t full[S];
+  __shared__ int abort_flag, n_issued;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(s_smem_raw) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int h = blockIdx.y, s = blockIdx.z, split = blockIdx.x;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) mbar_init(&full[i], 1);
+    abort_flag = n_issued = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
   tc::pdl_wait();
   tc::pdl_trigger();
   const Seq q = load_seq(a.ch, s);
@@ -208,50 +215,30 @@ __global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) 
   const int vecs = q.n * a.group;
   const Span keys = part_of(q.cached + q.n, split, a.splits, kSTile);
   const int n_tiles = (keys.hi - keys.lo + kSTile - 1) / kSTile;
+  __syncthreads();                                     // the barriers
 
-  const uint16_t* kp = static_cast<const uint16_t*>(a.kv.k) + a.layer * a.kv.layer_stride + h * a.kv.head_stride;
-  const uint16_t* vp = static_cast<const uint16_t*>(a.kv.v) + a.layer * a.kv.layer_stride + h * a.kv.head_stride;
+  // Tile t into its stage, by one warp: a lane per box (`rows` places of a page) and chunk of 64 dimensions, K and V.
   const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
-  const int chunk = threadIdx.x % kC, sub = threadIdx.x / kC;
-  // pages of the four 16-key groups of tile t (16 keys lie in one page)
-  auto pages_of = [&](int t, int (&pg)[4]) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int pos = keys.lo + t * kSTile + 16 * g;
-      pg[g] = t < n_tiles && pos < keys.hi ? __ldg(table + pos / a.kv.page_size) : 0;
+  const int rows = min(a.kv.page_size, kSTile), boxes = kSTile / rows;
+  const int my_box = lane / (2 * kDC), my_chunk = lane % kDC;
+  const bool my_v = lane / kDC & 1;
+  auto load_tile = [&](int t) {
+    const int pos = keys.lo + t * kSTile + my_box * rows;
+    const bool mine = my_box < boxes && pos < keys.hi;
+    int page = mine ? __ldg(table + pos / a.kv.page_size) : 0;
+    if (page < 0 || page >= a.kv.n_pages) {
+      report(a.err, MCD_ERR_INVALID_ARG);
+      page = 0;
     }
+    const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, mine)) * rows * 128u;
+    if (lane == 0) mbar_arrive_expect_tx(&full[t % S], bytes);
+    __syncwarp();
+    if (mine)
+      tma_page(smem + t % S * L::kStage + (my_v ? L::kHalf : 0) + my_chunk * kChunk + my_box * rows * 128, my_v ? &v_map : &k_map,
+               my_chunk * 64, pos % a.kv.page_size, h, page, &full[t % S]);
+    if (lane == 0) atomicMax(&n_issued, t + 1);
   };
-  auto copy_tile = [&](int t, const int (&pg)[4]) {
-    if (t < n_tiles) {
-      uint8_t* st = s_smem + t % L::kStages * L::kStage;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int pos0 = keys.lo + t * kSTile + 16 * g;
-        const bool ok = pg[g] >= 0 && pg[g] < a.kv.n_pages;
-        if (!ok && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
-        const long long base = ok ? pg[g] * a.kv.page_stride + pos0 % a.kv.page_size * a.kv.token_stride : 0;
-#pragma unroll
-        for (int r0 = 0; r0 < 16; r0 += kRows) {
-          const int r = r0 + sub, row = 16 * g + r;
-          const bool real = ok && pos0 + r < keys.hi;
-          const long long off = real ? base + r * a.kv.token_stride + chunk * 8 : 0;
-          const int at = row * (D * 2) + ((chunk ^ (row & 7)) << 4);
-          cpa16_or_zero(st + at, kp + off, real);
-          cpa16_or_zero(st + L::kHalf + at, vp + off, real);
-        }
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  int pg[4];
-  pages_of(0, pg);
-  copy_tile(0, pg);
-#pragma unroll
-  for (int t = 1; t < L::kStages - 1; ++t) {
-    pages_of(t, pg);
-    copy_tile(t, pg);
-  }
-  pages_of(L::kStages - 1, pg);
+  if (warp < min(S, n_tiles)) load_tile(warp);
 
   // the vectors as A fragments: rows lane / 4 and + 8, columns 2 (lane % 4) and + 8 of every 16
   uint4 qf[D / 16];
@@ -276,20 +263,27 @@ __global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) 
   // rows of the vectors (none: nobody reads what such a vector gives)
   const int i0 = r0 < vecs ? r0 / a.group : -1, i1 = r1 < vecs ? r1 / a.group : -1;
 
+  bool ok = true;
   for (int t = 0; t < n_tiles; ++t) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(L::kStages - 2) : "memory");
-    __syncthreads();                                   // tile t is in; tile t - 1 has been read
-    copy_tile(t + L::kStages - 1, pg);
-    pages_of(t + L::kStages, pg);
-    const uint32_t ks = smem_u32(s_smem + t % L::kStages * L::kStage), vs = ks + L::kHalf;
+    // (a wait that gave up: what follows is worthless, and reported; the CTA goes on in step and loads no more)
+    ok = ok && warp_wait(&full[t % S], t / S & 1, a.err, &abort_flag);
+    uint8_t* const v_tile = smem + t % S * L::kStage + L::kHalf;
+    const uint32_t vs = smem_u32(v_tile), ks = vs - L::kHalf;
     const int key0 = keys.lo + t * kSTile + 16 * warp;
+    if (key0 + 16 > keys.hi) {                         // values behind the keys: zeros
+      for (int i = max(0, keys.hi - key0) * 8 + lane; i < 16 * 8; i += 32)
+        for (int c = 0; c < kDC; ++c) *reinterpret_cast<uint4*>(v_tile + c * kChunk + 16 * warp * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+      __syncwarp();
+    }
     float z[2][4] = {};
     {
+      // (16-byte piece c of a row is at c ^ (row % 8))
       const int row = 16 * warp + (lane & 7) + ((lane & 16) >> 1);
+      const uint32_t at = ks + row * 128 + ((((lane >> 3) & 1) ^ (row & 7)) << 4);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         uint32_t b[4];
-        ldsm4(b, ks + row * (D * 2) + (((2 * i + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+        ldsm4(b, (at ^ (i & 3) << 5) + (i >> 2) * kChunk);
         mma_bf16_16816(z[0], qf[i], b[0], b[1]);
         mma_bf16_16816(z[1], qf[i], b[2], b[3]);
       }
@@ -344,21 +338,22 @@ __global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) 
     // the tile's new rows has such a value, the sums skip hidden keys one by one.
     bool odd = false;
     if (edge && __any_sync(0xffffffffu, hidden)) {
-      const int first = max(q.cached - key0, 0), n = (min(keys.hi - key0, 16) - first) * kC;
-      for (int i = lane; i < n; i += 32) {
-        const uint4 v = *reinterpret_cast<const uint4*>(s_smem + t % L::kStages * L::kStage + L::kHalf +
-                                                        (16 * warp + first + i / kC) * (D * 2) + (i % kC << 4));
-        odd |= !(bf16x2_finite(v.x) && bf16x2_finite(v.y) && bf16x2_finite(v.z) && bf16x2_finite(v.w));
-      }
+      const int first = max(q.cached - key0, 0), n = (min(keys.hi - key0, 16) - first) * 8;
+      for (int i = lane; i < n; i += 32)
+        for (int c = 0; c < kDC; ++c) {
+          const uint4 v = *reinterpret_cast<const uint4*>(v_tile + c * kChunk + (16 * warp + first) * 128 + i * 16);
+          odd |= !(bf16x2_finite(v.x) && bf16x2_finite(v.y) && bf16x2_finite(v.z) && bf16x2_finite(v.w));
+        }
       odd = __any_sync(0xffffffffu, odd);
     }
     if (!odd) {
       const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       const int row = 16 * warp + (lane & 15);
+      const uint32_t at = vs + row * 128 + (((lane >> 4) ^ (row & 7)) << 4);
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         uint32_t b[4];
-        ldsm4t(b, vs + row * (D * 2) + (((2 * i + (lane >> 4)) ^ (row & 7)) << 4));
+        ldsm4t(b, (at ^ (i & 3) << 5) + (i >> 2) * kChunk);
         mma_bf16_16816(o[2 * i], ph, b[0], b[1]);
         mma_bf16_16816(o[2 * i], pl, b[0], b[1]);
         mma_bf16_16816(o[2 * i + 1], ph, b[2], b[3]);
@@ -380,18 +375,24 @@ __global__ void __launch_bounds__(kSThreads) attn_step_kernel(const AttnArgs a) 
           }
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
-          const uint32_t v = *reinterpret_cast<const uint32_t*>(s_smem + t % L::kStages * L::kStage + L::kHalf + row * (D * 2) +
-                                                                ((i ^ (row & 7)) << 4) + 4 * (lane & 3));
+          const uint32_t v =
+              *reinterpret_cast<const uint32_t*>(v_tile + (i >> 3) * kChunk + row * 128 + (((i & 7) ^ (row & 7)) << 4) + 4 * (lane & 3));
           if (!ha) o[i][0] = fmaf(pa, bf16_lo_f32(v), o[i][0]), o[i][1] = fmaf(pa, bf16_hi_f32(v), o[i][1]);
           if (!hb) o[i][2] = fmaf(pb, bf16_lo_f32(v), o[i][2]), o[i][3] = fmaf(pb, bf16_hi_f32(v), o[i][3]);
         }
       }
     }
+    __syncthreads();                                   // the tile has been read: its stage takes tile t + S
+    if (t + S < n_tiles && warp == (t & 3) && !*(volatile int*)&abort_flag) load_tile(t + S);
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
+  if (abort_flag) {                                    // copies that were late land before their place is used again
+    if (warp == 0)
+      for (int t = max(0, n_issued - S); t < n_issued; ++t) tc::tc_wait(&full[t % S], t / S & 1, a.err, 2000000000ull);
+    __syncthreads();
+  }
   // the four warps' parts, then their sum over the first one's place
-  float* os = reinterpret_cast<float*>(s_smem);
+  float* os = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int w = 1; w < 4; w <<= 1) {
     l0 += __shfl_xor_sync(0xffffffffu, l0, w);
@@ -507,13 +508,16 @@ StepPlan plan_step(const mcd_paged_kv& kv, const mcd_chunks& ch) {
 template <int D>
 cudaError_t launch_step(AttnArgs a, void* workspace, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
-  const int bytes = SLayout<D>::kBytes;
+  const int bytes = SLayout<D>::kBytes, rows = std::min(a.kv.page_size, kSTile);
   cudaError_t e = opt_in(attn_step_kernel<D>, bytes, done);
   if (e != cudaSuccess) return e;
+  CUtensorMap k_map, v_map;
+  if (!page_map(&k_map, a.kv, a.kv.k, a.layer, rows) || !page_map(&v_map, a.kv, a.kv.v, a.layer, rows)) return cudaErrorInvalidValue;
   const StepPlan p = plan_step(a.kv, a.ch);
   a.splits = p.splits;
   a.part = p.in_workspace ? static_cast<float*>(workspace) : nullptr;
-  e = launch_clusters(attn_step_kernel<D>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a);
+  e = launch_clusters(attn_step_kernel<D>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a, k_map,
+                      v_map);
   if (e == cudaSuccess && a.part) e = tc::launch(true, attn_join_kernel<D>, dim3(a.kv.n_kv_heads, a.ch.n_seqs), dim3(256), 0, st, a);
   return e;
 }

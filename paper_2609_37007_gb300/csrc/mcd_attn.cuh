@@ -11,6 +11,7 @@
 // of one (sequence, KV head).
 #pragma once
 #include <cooperative_groups.h>
+#include <cuda.h>
 
 #include "mcd_cache.cuh"
 
@@ -89,6 +90,35 @@ __device__ __forceinline__ Span part_of(int n_keys, int z, int splits, int tile)
   return {(int)lo, (int)min((long long)n_keys, lo + per)};
 }
 
+// A warp's bounded wait (the same answer in every lane).  The test alone where the phase is over: a look at the abort
+// flag beside it doubled the 64 cycles that it takes, six times a pair of tiles in the warp that issues.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* abort_flag) {
+  constexpr unsigned long long kWait = 2000000000ull;
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  const uint64_t t0 = globaltimer();
+  for (int n = 1;; ++n) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (n % 16) continue;
+    const bool given_up = *abort_flag != 0, late = globaltimer() - t0 > kWait;
+    if (__any_sync(0xffffffffu, given_up || late)) {
+      if ((threadIdx.x & 31) == 0) {
+        if (!given_up) report(err, MCD_ERR_TIMEOUT);
+        *abort_flag = 1;
+      }
+      return false;
+    }
+  }
+}
+
+// Box of a page: places t0 .. of KV head h, dimensions d .. d + 63, in 128-byte swizzled rows.
+__device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int d, int t0, int h, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_u32(dst)),
+      "l"(map), "r"(d), "r"(t0), "r"(h), "r"(page), "r"(smem_u32(bar))
+      : "memory");
+}
+
 // Joins the parts of `vecs` packed vectors (from p0 on) that the CTAs of a cluster hold in the same places of their shared
 // memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
 // m = -inf and l = 0; nothing at all gives zeros.
@@ -153,6 +183,9 @@ cudaError_t opt_in(K* kernel, int bytes, std::atomic<unsigned>& done) {
   if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
   return e;
 }
+
+// Tensor map of one layer's pages for tma_page, boxes of `rows` places (false: no driver).
+bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int layer, int rows);
 
 // Sequences with more than a.least_vecs packed vectors, bf16 (mcd_attn_chunk.cu).
 cudaError_t launch_chunk(const AttnArgs& a, cudaStream_t st);

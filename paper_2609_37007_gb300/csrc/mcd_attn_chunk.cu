@@ -15,8 +15,6 @@
 //                     such a pair of tiles is computed again, key by key)
 // What bounds it: for long prompts the tensor cores, 4 * 128 * 128 * D flop per pair of tiles and key tile
 // at 8192 flop a cycle and SM; the softmax needs about half of that time on the other pipes.
-#include <cuda.h>
-
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -44,14 +42,6 @@ struct CLayout {
   static_assert(kCRows * kPitch * 4 <= kBar, "the parts of o take the tiles' place");
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
-
-__device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int d, int h, int page, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-          smem_u32(dst)),
-      "l"(map), "r"(d), "r"(0), "r"(h), "r"(page), "r"(smem_u32(bar))
-      : "memory");
-}
 
 // B = V: D[m][n] += A[m][k] V[k][n], V in rows of 64 n (128 swizzled bytes), k the row: the n-major layout.  16 k
 // are two groups of 8 rows, 1024 bytes apart; the next 64 n are `chunk` bytes on.
@@ -100,26 +90,6 @@ __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
   return p != 0;
-}
-
-// A warp's bounded wait (the same answer in every lane).  The test alone where the phase is over: a look at the abort
-// flag beside it doubled the 64 cycles that it takes, six times a pair of tiles in the warp that issues.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* err, volatile int* abort_flag) {
-  constexpr unsigned long long kWait = 2000000000ull;
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  const uint64_t t0 = globaltimer();
-  for (int n = 1;; ++n) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if (n % 16) continue;
-    const bool given_up = *abort_flag != 0, late = globaltimer() - t0 > kWait;
-    if (__any_sync(0xffffffffu, given_up || late)) {
-      if ((threadIdx.x & 31) == 0) {
-        if (!given_up) report(err, MCD_ERR_TIMEOUT);
-        *abort_flag = 1;
-      }
-      return false;
-    }
-  }
 }
 
 // Two fp32 operations an instruction.
@@ -305,7 +275,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         }
         go = __shfl_sync(0xffffffffu, (int)go, 0);
         if (!go) break;
-        if (mine) tma_page(stage(i) + chunk * kChunk + box * a.kv.page_size * 128, kv ? &v_map : &k_map, chunk * 64, h, page, load_bar(i));
+        if (mine) tma_page(stage(i) + chunk * kChunk + box * a.kv.page_size * 128, kv ? &v_map : &k_map, chunk * 64, 0, h, page, load_bar(i));
       }
       if (!go) break;
     }
@@ -603,25 +573,14 @@ EncodeTiled encoder() {
   return reinterpret_cast<EncodeTiled>(fn);
 }
 
-// Boxes of one page's places x 64 dimensions of one head.
-bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int layer) {
-  const EncodeTiled encode = encoder();
-  if (!encode) return false;
-  void* base = static_cast<uint8_t*>(const_cast<void*>(pool)) + layer * kv.layer_stride * 2;
-  const cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)kv.token_stride * 2, (cuuint64_t)kv.head_stride * 2, (cuuint64_t)kv.page_stride * 2};
-  const cuuint32_t box[4] = {64, (cuuint32_t)kv.page_size, 1, 1}, one[4] = {1, 1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
   cudaError_t e = opt_in(attn_chunk_kernel<D>, CLayout<D>::kBytes, done);
   if (e != cudaSuccess) return e;
   CUtensorMap k_map, v_map;
-  if (!page_map(&k_map, a.kv, a.kv.k, a.layer) || !page_map(&v_map, a.kv, a.kv.v, a.layer)) return cudaErrorInvalidValue;
+  if (!page_map(&k_map, a.kv, a.kv.k, a.layer, a.kv.page_size) ||
+      !page_map(&v_map, a.kv, a.kv.v, a.layer, a.kv.page_size)) return cudaErrorInvalidValue;
   const long long slots = (long long)a.ch.n_rows * a.group / kCRows + a.ch.n_seqs;
   const long long pairs = std::min(slots, a.ch.n_seqs * (((long long)a.ch.max_rows * a.group + kCRows - 1) / kCRows));
   // one CTA an SM: parts as long as they leave no SM two, each of two tiles at least
@@ -634,6 +593,17 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
 }
 
 }  // namespace
+
+bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int layer, int rows) {
+  const EncodeTiled encode = encoder();
+  if (!encode) return false;
+  void* base = static_cast<uint8_t*>(const_cast<void*>(pool)) + layer * kv.layer_stride * 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)kv.token_stride * 2, (cuuint64_t)kv.head_stride * 2, (cuuint64_t)kv.page_stride * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 cudaError_t launch_chunk(const AttnArgs& a, cudaStream_t st) {
   return a.kv.head_dim == 64 ? launch_chunk_d<64>(a, st) : launch_chunk_d<128>(a, st);
