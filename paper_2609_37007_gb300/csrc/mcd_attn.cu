@@ -32,17 +32,16 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   const int z = blockIdx.x % a.splits;
-  const long long vecs = (long long)max(q.n, 0) * a.group, p0 = (long long)(blockIdx.x / a.splits) * kBM;
+  const int vecs = max(q.n, 0) * a.group, p0 = blockIdx.x / a.splits * kBM;
   if (p0 >= vecs) return;                              // (all CTAs of the cluster alike)
-  const int last_row = (int)min((long long)q.n - 1, (p0 + kBM - 1) / a.group);
+  const Pack pack(p0, a.group);
+  const int live = min(kBM, vecs - p0), last_row = pack.row(live - 1);
   const Span keys = part_of(a.mask ? q.cached + q.n : q.cached + last_row + 1, z, a.splits, kFN);
 
   for (int i = threadIdx.x; i < kBM * (D / 4); i += kFThreads) {
     const int r = i / (D / 4), d = i % (D / 4) * 4;
-    const long long p = p0 + r;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p < vecs)
-      x = load4(static_cast<const float*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + d);
+    if (r < live) x = load4(static_cast<const float*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + d);
     *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
   }
   float m[RM], l[RM];
@@ -91,7 +90,7 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
     const bool edge = k0 + kFN > q.cached;             // some key of the tile may be hidden from some row
 #pragma unroll
     for (int r = 0; r < RM; ++r) {
-      const int row = (int)((p0 + ty * RM + r) / a.group);
+      const int row = pack.row(ty * RM + r);
       bool see[4];
       float mx = -INFINITY;
 #pragma unroll
@@ -150,17 +149,17 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       for (int c = 0; c < kDC; ++c) *reinterpret_cast<float4*>(&os[ty * RM + r][tx * 4 + 64 * c]) = o[r][c];
       if (tx == 0) sm.m[ty * RM + r] = m[r], sm.l[ty * RM + r] = l[r];
     }
-    join_cluster<float, D>(a, q, h, p0, (int)min((long long)kBM, vecs - p0), &os[0][0], D + 4, sm.m, sm.l);
+    join_cluster<float, D>(a, q, h, pack, live, &os[0][0], D + 4, sm.m, sm.l);
     return;
   }
 #pragma unroll
   for (int r = 0; r < RM; ++r) {
-    const long long p = p0 + ty * RM + r;
-    if (p >= vecs) continue;
+    if (ty * RM + r >= live) continue;
     const float f = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
     for (int c = 0; c < kDC; ++c)
-      store4(out_at<float, D>(a, q, h, p, tx * 4 + 64 * c), make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
+      store4(static_cast<float*>(a.out) + vec_at<D>(pack, q, h, ty * RM + r, a.out_stride) + tx * 4 + 64 * c,
+             make_float4(o[r][c].x * f, o[r][c].y * f, o[r][c].z * f, o[r][c].w * f));
   }
 }
 
@@ -213,6 +212,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
   if (q.n < 0 && split == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   if (q.n <= 0 || q.n > kSVecs / a.group) return;      // (more: the chunk kernel's)
   const int vecs = q.n * a.group;
+  const Pack pack(0, a.group);
   const Span keys = part_of(q.cached + q.n, split, a.splits, kSTile);
   const int n_tiles = (keys.hi - keys.lo + kSTile - 1) / kSTile;
   __syncthreads();                                     // the barriers
@@ -244,9 +244,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
   uint4 qf[D / 16];
   const int r0 = lane >> 2, r1 = r0 + 8;
   {
-    auto ptr = [&](int p) {
-      return static_cast<const uint16_t*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + 2 * (lane & 3);
-    };
+    auto ptr = [&](int p) { return static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, p, a.q_stride) + 2 * (lane & 3); };
     const uint16_t *q0 = ptr(min(r0, vecs - 1)), *q1 = ptr(min(r1, vecs - 1));
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
@@ -261,7 +259,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
   for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
   // rows of the vectors (none: nobody reads what such a vector gives)
-  const int i0 = r0 < vecs ? r0 / a.group : -1, i1 = r1 < vecs ? r1 / a.group : -1;
+  const int i0 = r0 < vecs ? pack.row(r0) : -1, i1 = r1 < vecs ? pack.row(r1) : -1;
 
   bool ok = true;
   for (int t = 0; t < n_tiles; ++t) {
@@ -422,7 +420,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
     }
     if (a.splits == 1) {
       const float f = sum == 0.f ? 0.f : 1.f / sum;
-      store4(out_at<uint16_t, D>(a, q, h, r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+      store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
     } else if (a.part) {
       float* to = a.part + ((pair * a.splits + split) * kSVecs + r) * (D + 4);
       *reinterpret_cast<float4*>(to + d) = x;
@@ -432,7 +430,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
       if (d == 0) fin_m[r] = mx, fin_l[r] = sum;
     }
   }
-  if (a.splits > 1 && !a.part) join_cluster<uint16_t, D>(a, q, h, 0, vecs, os, L::kPitch, fin_m, fin_l);
+  if (a.splits > 1 && !a.part) join_cluster<uint16_t, D>(a, q, h, pack, vecs, os, L::kPitch, fin_m, fin_l);
 }
 
 // Joins parts in the workspace: a CTA per (KV head, sequence), a thread per four elements of o.
@@ -444,6 +442,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
   const Seq q = load_seq(a.ch, s);
   if (q.n <= 0 || q.n > kSVecs / a.group) return;
   const int vecs = q.n * a.group;
+  const Pack pack(0, a.group);
   const long long pair = (long long)s * a.kv.n_kv_heads + h;
   for (int t = threadIdx.x; t < vecs * (D / 4); t += 256) {
     const int r = t / (D / 4), d = t % (D / 4) * 4;
@@ -463,7 +462,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
       x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     }
     const float f = sum == 0.f ? 0.f : 1.f / sum;
-    store4(out_at<uint16_t, D>(a, q, h, r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+    store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
 }
 
@@ -548,7 +547,7 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
       !std::isfinite(scale))
     return MCD_ERR_INVALID_ARG;
   if (mask && (int64_t)mask_words * 32 < chunks->max_rows) return MCD_ERR_INVALID_ARG;
-  if (n_q_heads / kv->n_kv_heads > 16) return MCD_ERR_UNSUPPORTED;
+  if (n_q_heads / kv->n_kv_heads > 16 || (int64_t)chunks->n_rows * 16 > INT32_MAX) return MCD_ERR_UNSUPPORTED;
   if (no_rows(chunks)) return MCD_OK;
   if (!q || !out || q == out) return MCD_ERR_INVALID_ARG;
   const int64_t width = (int64_t)n_q_heads * kv->head_dim;

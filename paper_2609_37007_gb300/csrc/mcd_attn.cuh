@@ -74,10 +74,19 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
 }
 
-// Output element of packed vector p, dimension d.
-template <class T, int D>
-__device__ __forceinline__ T* out_at(const AttnArgs& a, const Seq& q, int h, long long p, int d) {
-  return static_cast<T*>(a.out) + (q.row0 + p / a.group) * a.out_stride + (h * a.group + p % a.group) * D + d;
+// Packed vectors p0 + r of a tile (r < 4096): row of the sequence and head of the group without a division each
+// (64-bit divisions in the loads of Q had taken 40,000 cycles a CTA).  floor(t / group) = t ceil(2^16 / group) >> 16
+// for t < 2^16 / group.
+struct Pack {
+  int row0, head0, inverse, group;
+  __device__ __forceinline__ Pack(int p0, int group) : row0(p0 / group), head0(p0 - row0 * group), inverse((65535 + group) / group), group(group) {}
+  __device__ __forceinline__ int row(int r) const { return row0 + ((head0 + r) * inverse >> 16); }
+  __device__ __forceinline__ int head(int r) const { return head0 + r - ((head0 + r) * inverse >> 16) * group; }
+};
+// Elements of vector r in rows of `stride` elements.
+template <int D>
+__device__ __forceinline__ long long vec_at(const Pack& v, const Seq& q, int h, int r, long long stride) {
+  return (q.row0 + v.row(r)) * stride + (h * v.group + v.head(r)) * D;
 }
 
 // Part z of the keys [0, n_keys), in whole tiles of `tile` keys.
@@ -119,11 +128,11 @@ __device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int 
       : "memory");
 }
 
-// Joins the parts of `vecs` packed vectors (from p0 on) that the CTAs of a cluster hold in the same places of their shared
+// Joins the parts of `vecs` packed vectors that the CTAs of a cluster hold in the same places of their shared
 // memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
 // m = -inf and l = 0; nothing at all gives zeros.
 template <class T, int D>
-__device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, long long p0, int vecs, float* o, int pitch,
+__device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, const Pack& pack, int vecs, float* o, int pitch,
                                              float* m, float* l) {
   namespace cg = cooperative_groups;
   cg::cluster_group cl = cg::this_cluster();
@@ -143,7 +152,7 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, in
       x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
     }
     const float f = sum == 0.f ? 0.f : 1.f / sum;
-    store4(out_at<T, D>(a, q, h, p0 + r, d), make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
+    store4(static_cast<T*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
   cl.sync();                                           // nobody leaves while others read
 }

@@ -136,13 +136,13 @@ __device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, i
   return __funnelshift_r(__ldg(row + w), next, j0 & 31) & in;
 }
 
-// One packed vector over the keys of `keys`, key by key, by a warp; lane d holds dimensions d * D / 32 ...
+// Packed vector r of the pair over the keys of `keys`, key by key, by a warp; lane d holds dimensions d * D / 32 ...
 template <int D>
-__device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, long long p, Span keys, float& m, float& l,
+__device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, const Pack& pack, int r, Span keys, float& m, float& l,
                                       float (&o)[D / 32]) {
   constexpr int kE = D / 32;
-  const int lane = threadIdx.x & 31, i = (int)(p / a.group);
-  const uint16_t* qp = static_cast<const uint16_t*>(a.q) + (q.row0 + p / a.group) * a.q_stride + (h * a.group + p % a.group) * D + lane * kE;
+  const int lane = threadIdx.x & 31, i = pack.row(r);
+  const uint16_t* qp = static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + lane * kE;
   float x[kE];
   for (int e = 0; e < kE; ++e) x[e] = bf16_bits_to_f32(qp[e]), o[e] = 0.f;
   m = -INFINITY, l = 0.f;
@@ -194,18 +194,20 @@ __global__ void __launch_bounds__(kCThreads, 1)
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.ch.n_seqs; i += kCThreads)
       if (load_seq(a.ch, i).n < 0) report(a.err, MCD_ERR_INVALID_ARG);
-  const long long vecs = (long long)max(q.n, 0) * a.group, n_pairs = (vecs + kCRows - 1) / kCRows, local = slot - first_slot(s);
+  const int vecs = max(q.n, 0) * a.group, n_pairs = (vecs + kCRows - 1) / kCRows;
+  const long long local = slot - first_slot(s);
   // (all CTAs of a cluster decide alike; few vectors: the step kernel's)
   if (local < 0 || local >= n_pairs || vecs <= a.least_vecs) return;
-  const long long p0 = (n_pairs - 1 - local) * kCRows;
-  const int i_first = (int)(p0 / a.group);
-  auto keys_below = [&](long long p1) {                // keys that some vector below p1 sees
-    return a.mask ? q.cached + q.n : q.cached + (int)((min(p1, vecs) - 1) / a.group) + 1;
+  const int p0 = (n_pairs - 1 - (int)local) * kCRows;
+  const Pack pack(p0, a.group);
+  const int i_first = pack.row0, n_vecs = min(kCRows, vecs - p0);
+  auto keys_below = [&](int r) {                       // keys that some vector of the pair below r sees
+    return a.mask ? q.cached + q.n : q.cached + pack.row(min(r, n_vecs) - 1) + 1;
   };
-  const bool two = p0 + kCTile < vecs;                 // tile b has rows
-  const Span keys = part_of(keys_below(p0 + (two ? kCRows : kCTile)), part, a.splits, kCTile);
+  const bool two = kCTile < n_vecs;                    // tile b has rows
+  const Span keys = part_of(keys_below(kCRows), part, a.splits, kCTile);
   auto tiles_of = [&](int hi) { return max(0, (min(hi, keys.hi) - keys.lo + kCTile - 1) / kCTile); };
-  const int n_tiles = tiles_of(keys.hi), n_a = tiles_of(keys_below(p0 + kCTile)), n_b = two ? n_tiles : 0;
+  const int n_tiles = tiles_of(keys.hi), n_a = tiles_of(keys_below(kCTile)), n_b = two ? n_tiles : 0;
   // Tiles whose V warp 10 looks at, from this one on: those that end behind the keys or hold a key that some row does
   // not see.  Number n of these has barriers n % (S / 2) of its own (no more V tiles are in the ring): warp 10 waits
   // for every phase of them, as it could not for the ring's, whose earlier phases it has no part in.
@@ -363,27 +365,25 @@ __global__ void __launch_bounds__(kCThreads, 1)
     // ---- softmax: thread t of tile w has row t
     const int w = warp >> 2, t = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const long long p = p0 + w * kCTile + t;
     // Q rows into shared memory, D / 8 lanes a row
     {
       constexpr int kC = D / 8;
       for (int n = t; n < kCTile * kC; n += 128) {
         const int r = n / kC, c = n % kC;
-        const long long pp = p0 + w * kCTile + r;
         uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (pp < vecs)
-          x = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + (q.row0 + pp / a.group) * a.q_stride +
-                                                   (h * a.group + pp % a.group) * D + c * 8));
+        if (w * kCTile + r < n_vecs)
+          x = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, w * kCTile + r, a.q_stride) + c * 8));
         *reinterpret_cast<uint4*>(smem + w * L::kTileBytes + tc::sw128_offset(kCTile, r, c >> 3, c & 7)) = x;
       }
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
     }
-    const int n_mine = w ? n_b : n_a, row = (int)(min(p, vecs - 1) / a.group);
-    const bool live = p0 + w * kCTile + (warp & 3) * 32 < vecs;           // the warp has rows
+    const int n_mine = w ? n_b : n_a, mine = w * kCTile + t, row = pack.row(min(mine, n_vecs - 1));
+    const int base = w * kCTile + (warp & 3) * 32;     // the warp's first vector
+    const bool live = base < n_vecs;
     // keys below this position are seen by every row of the warp
-    const int clear = q.cached + (a.mask ? 0 : (int)((p0 + w * kCTile + (warp & 3) * 32) / a.group) + 1);
+    const int clear = q.cached + (a.mask ? 0 : pack.row(base) + 1);
     float mc = 0.f;                                    // c * (the maximum in use)
     bool ok = true;
     for (int j = 0; j < n_mine; ++j) {
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         // (m is -inf until the row has seen a key: then any is growth)
         const bool grown = top * a.c > m + kGrowth || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, grown)) {
-          const float n = fmaxf(m, top * a.c), base = n == -INFINITY ? 0.f : n, f = ex2(m - base);
+          const float n = fmaxf(m, top * a.c), from = n == -INFINITY ? 0.f : n, f = ex2(m - from);
           if (j > 0) {                                   // (S of tile j came after the product with P of tile j - 1)
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {          // (few columns at a time: S fills the registers)
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
           }
           l *= f;
           m = n;
-          mc = base;
+          mc = from;
         }
         const uint64_t scale = pack2(a.c, a.c), shift = pack2(-mc, -mc);
         uint64_t sum[2] = {0ull, 0ull};                // (two zeros each)
@@ -482,23 +482,22 @@ __global__ void __launch_bounds__(kCThreads, 1)
     if (a.splits == 1 && ok && live) {
       if (__any_sync(0xffffffffu, *odd)) {
         for (int r = 0; r < 32; ++r) {
-          const long long pp = p0 + w * kCTile + (warp & 3) * 32 + r;
-          if (pp >= vecs) break;
+          if (base + r >= n_vecs) break;
           float sl, sm, o[D / 32];
-          slow_row<D>(a, q, s, h, pp, keys, sm, sl, o);
+          slow_row<D>(a, q, s, h, pack, base + r, keys, sm, sl, o);
           const float f = sl == 0.f ? 0.f : 1.f / sl;
-          uint16_t* to = out_at<uint16_t, D>(a, q, h, pp, lane * (D / 32));
+          uint16_t* to = static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, base + r, a.out_stride) + lane * (D / 32);
           for (int e = 0; e < D / 32; ++e) to[e] = (uint16_t)pack_bf16x2(o[e] * f, 0.f);
         }
       } else {
         const float f = l == 0.f ? 0.f : 1.f / l;
-        uint16_t* to = out_at<uint16_t, D>(a, q, h, min(p, vecs - 1), 0);
+        uint16_t* to = static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, min(mine, n_vecs - 1), a.out_stride);
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t y[32];
           tmem_ld32(o_col(w) + lanes + c, y);
           tmem_loaded(y);
-          if (p < vecs) {
+          if (mine < n_vecs) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8) {
               uint32_t z[4];
@@ -521,11 +520,11 @@ __global__ void __launch_bounds__(kCThreads, 1)
       const int w = warp >> 2, t = threadIdx.x & 127, r = w * kCTile + t, n_mine = w ? n_b : n_a;
       const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
       const int base = w * kCTile + (warp & 3) * 32;
-      const bool some = n_mine > 0 && !*abort_flag && p0 + base < vecs;
+      const bool some = n_mine > 0 && !*abort_flag && base < n_vecs;
       if (some && *odd) {
-        for (int n = 0; n < 32 && p0 + base + n < vecs; ++n) {
+        for (int n = 0; n < 32 && base + n < n_vecs; ++n) {
           float sm, sl, o[D / 32];
-          slow_row<D>(a, q, s, h, p0 + base + n, keys, sm, sl, o);
+          slow_row<D>(a, q, s, h, pack, base + n, keys, sm, sl, o);
           for (int e = 0; e < D / 32; ++e) os[(base + n) * L::kPitch + lane * (D / 32) + e] = o[e];
           if (lane == 0) sm_m[base + n] = sm, sm_l[base + n] = sl;
         }
@@ -546,7 +545,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         sm_l[r] = some ? l : 0.f;
       }
     }
-    join_cluster<uint16_t, D>(a, q, h, p0, (int)min((long long)kCRows, vecs - p0), os, L::kPitch, sm_m, sm_l);
+    join_cluster<uint16_t, D>(a, q, h, pack, n_vecs, os, L::kPitch, sm_m, sm_l);
     tc::tc_fence_before();
     __syncthreads();
   }
