@@ -43,6 +43,15 @@ struct CLayout {
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
+// Box of rows of Q: dimensions d .. d + 63 of the heads from h0 on, rows from row0 on.
+__device__ __forceinline__ void tma_rows(void* dst, const CUtensorMap* map, int d, int h0, int row0, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"(map), "r"(d), "r"(h0), "r"(row0), "r"(smem_u32(bar))
+      : "memory");
+}
+
 // B = V: D[m][n] += A[m][k] V[k][n], V in rows of 64 n (128 swizzled bytes), k the row: the n-major layout.  16 k
 // are two groups of 8 rows, 1024 bytes apart; the next 64 n are `chunk` bytes on.
 __device__ __forceinline__ uint64_t v_desc(uint32_t addr, uint32_t chunk) {
@@ -165,7 +174,8 @@ __device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, in
 
 template <int D>
 __global__ void __launch_bounds__(kCThreads, 1)
-    attn_chunk_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    attn_chunk_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                      const __grid_constant__ CUtensorMap q_map, const int q_boxes) {
   using L = CLayout<D>;
   constexpr int S = L::kStages, kDC = D / 64;          // 64-dimension chunks of a row
   constexpr uint32_t kChunk = kCTile * 128;            // bytes of one chunk of a tile
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    mbar_init(q_full, 8);
+    mbar_init(q_full, q_boxes ? 1 : 8);
     mbar_init(drain, 1);
     for (int w = 0; w < 2; ++w) {
       mbar_init(&s_full[w], 1);
@@ -258,6 +268,13 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
     const int box = lane / kDC, chunk = lane % kDC;
     uint32_t i = 0;
+    if (q_boxes && n_tiles > 0 && lane == 0) {         // Q: a box is the group's heads of kCTile / group rows, packed as it lies
+      mbar_arrive_expect_tx(q_full, (two ? 2 : 1) * L::kTileBytes);
+      for (int w = 0; w < (two ? 2 : 1); ++w)
+        for (int c = 0; c < kDC; ++c)
+          tma_rows(smem + w * L::kTileBytes + c * kChunk, &q_map, c * 64, h * a.group, q.row0 + pack.row(w * kCTile), q_full);
+    }
+    __syncwarp();
     for (int j = 0; j < n_tiles; ++j) {
       const int pos = keys.lo + j * kCTile + box * a.kv.page_size;
       const bool mine = box < boxes && pos < keys.hi;
@@ -282,6 +299,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
       if (!go) break;
     }
     // every copy lands before the CTA may end
+    if (lane == 0 && q_boxes && n_tiles > 0) tc::tc_wait(q_full, 0, a.err, kWait);
     if (lane == 0)
       for (uint32_t n = i > (uint32_t)S ? i - S : 0u; n < i; ++n) tc::tc_wait(load_bar(n), load_phase(n), a.err, kWait);
   } else if (warp == 9) {
@@ -365,16 +383,21 @@ __global__ void __launch_bounds__(kCThreads, 1)
     // ---- softmax: thread t of tile w has row t
     const int w = warp >> 2, t = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    // Q rows into shared memory, D / 8 lanes a row
-    {
+    // Q rows into shared memory where no box holds a tile (the group does not divide it), D / 8 lanes a row
+    if (!q_boxes) {
       constexpr int kC = D / 8;
-      for (int n = t; n < kCTile * kC; n += 128) {
-        const int r = n / kC, c = n % kC;
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (w * kCTile + r < n_vecs)
-          x = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, w * kCTile + r, a.q_stride) + c * 8));
-        *reinterpret_cast<uint4*>(smem + w * L::kTileBytes + tc::sw128_offset(kCTile, r, c >> 3, c & 7)) = x;
+      uint4 x[kC];                                     // all in flight: one after another they took 20 us
+#pragma unroll
+      for (int i = 0; i < kC; ++i) {
+        const int r = w * kCTile + i * (128 / kC) + t / kC;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < n_vecs)
+          x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + t % kC * 8));
       }
+#pragma unroll
+      for (int i = 0; i < kC; ++i)
+        *reinterpret_cast<uint4*>(smem + w * L::kTileBytes +
+                                  tc::sw128_offset(kCTile, i * (128 / kC) + t / kC, t % kC >> 3, t % kC & 7)) = x[i];
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full);
@@ -572,6 +595,17 @@ EncodeTiled encoder() {
   return reinterpret_cast<EncodeTiled>(fn);
 }
 
+// Rows of Q, boxes of a tile.
+bool rows_map(CUtensorMap* map, const AttnArgs& a) {
+  const EncodeTiled encode = encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)a.kv.head_dim, (cuuint64_t)a.kv.n_kv_heads * a.group, (cuuint64_t)a.ch.n_rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)a.kv.head_dim * 2, (cuuint64_t)a.q_stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(kCTile / a.group)}, one[3] = {1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
@@ -580,6 +614,10 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   CUtensorMap k_map, v_map;
   if (!page_map(&k_map, a.kv, a.kv.k, a.layer, a.kv.page_size) ||
       !page_map(&v_map, a.kv, a.kv.v, a.layer, a.kv.page_size)) return cudaErrorInvalidValue;
+  // Q by boxes where a tile is whole rows of the group's heads
+  CUtensorMap q_map = k_map;
+  const int q_boxes = kCTile % a.group == 0;
+  if (q_boxes && !rows_map(&q_map, a)) return cudaErrorInvalidValue;
   const long long slots = (long long)a.ch.n_rows * a.group / kCRows + a.ch.n_seqs;
   const long long pairs = std::min(slots, a.ch.n_seqs * (((long long)a.ch.max_rows * a.group + kCRows - 1) / kCRows));
   // one CTA an SM: parts as long as they leave no SM two, each of two tiles at least
@@ -588,7 +626,7 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
     a.splits *= 2;
   const long long grid = slots * a.kv.n_kv_heads * a.splits;
   if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  return launch_clusters(attn_chunk_kernel<D>, dim3((unsigned)grid), kCThreads, a.splits, CLayout<D>::kBytes, st, a, k_map, v_map);
+  return launch_clusters(attn_chunk_kernel<D>, dim3((unsigned)grid), kCThreads, a.splits, CLayout<D>::kBytes, st, a, k_map, v_map, q_map, q_boxes);
 }
 
 }  // namespace
