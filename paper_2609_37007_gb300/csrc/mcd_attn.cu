@@ -32,17 +32,26 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   const int z = blockIdx.x % a.splits;
-  const int vecs = max(q.n, 0) * a.group, p0 = blockIdx.x / a.splits * kBM;
+  // (the last tiles see most keys: they come first)
+  const int vecs = max(q.n, 0) * a.group, p0 = (gridDim.x / a.splits - 1 - blockIdx.x / a.splits) * kBM;
   if (p0 >= vecs) return;                              // (all CTAs of the cluster alike)
   const Pack pack(p0, a.group);
   const int live = min(kBM, vecs - p0), last_row = pack.row(live - 1);
   const Span keys = part_of(a.mask ? q.cached + q.n : q.cached + last_row + 1, z, a.splits, kFN);
 
-  for (int i = threadIdx.x; i < kBM * (D / 4); i += kFThreads) {
-    const int r = i / (D / 4), d = i % (D / 4) * 4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < live) x = load4(static_cast<const float*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + d);
-    *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
+  {
+    float4 x[RM * D / 64];                             // all loads in flight
+#pragma unroll
+    for (int i = 0; i < RM * D / 64; ++i) {
+      const int n = threadIdx.x + i * kFThreads, r = n / (D / 4);
+      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < live) x[i] = load4(static_cast<const float*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + n % (D / 4) * 4);
+    }
+#pragma unroll
+    for (int i = 0; i < RM * D / 64; ++i) {
+      const int n = threadIdx.x + i * kFThreads;
+      *reinterpret_cast<float4*>(&sm.q[n / (D / 4)][n % (D / 4) * 4]) = x[i];
+    }
   }
   float m[RM], l[RM];
   float4 o[RM][kDC];
@@ -53,22 +62,32 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < kDC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kFN * (D / 4); i += kFThreads) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-      if (k0 + r < keys.hi) {
-        const long long at = key_at(a, s, h, k0 + r);
-        if (at >= 0) {
-          x = load4(static_cast<const float*>(a.kv.k) + at + d);
-          y = load4(static_cast<const float*>(a.kv.v) + at + d);
-        }
+  // Tiles travel through registers: the next one is on its way while this one is multiplied.
+  constexpr int kPieces = kFN * (D / 4) / kFThreads, kStep = kFThreads / (D / 4);    // float4 a thread, rows between them
+  const int my_row = threadIdx.x / (D / 4), my_d = threadIdx.x % (D / 4) * 4;
+  float4 kn[kPieces], vn[kPieces];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      kn[i] = vn[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      const int pos = k0 + my_row + i * kStep;
+      const long long at = pos < keys.hi ? key_at(a, s, h, pos) : -1;
+      if (at >= 0) {
+        kn[i] = load4(static_cast<const float*>(a.kv.k) + at + my_d);
+        vn[i] = load4(static_cast<const float*>(a.kv.v) + at + my_d);
       }
-      *reinterpret_cast<float4*>(&sm.k[r][d]) = x;
-      *reinterpret_cast<float4*>(&sm.v[r][d]) = y;
+    }
+  };
+  fetch(keys.lo);
+  for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
+    __syncthreads();                                   // the tile before has been read
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      *reinterpret_cast<float4*>(&sm.k[my_row + i * kStep][my_d]) = kn[i];
+      *reinterpret_cast<float4*>(&sm.v[my_row + i * kStep][my_d]) = vn[i];
     }
     __syncthreads();
+    if (k0 + kFN < keys.hi) fetch(k0 + kFN);
     float sc[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
@@ -115,21 +134,27 @@ __global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
       for (int c = 0; c < kDC; ++c) o[r][c].x *= f, o[r][c].y *= f, o[r][c].z *= f, o[r][c].w *= f;
     }
     __syncwarp();
-    const int nk = min(kFN, keys.hi - k0);
-    for (int j = 0; j < nk; ++j) {
-      float4 vv[kDC];
+#pragma unroll 4
+    for (int j = 0; j < kFN; j += 4) {                 // (keys behind the end: p = -0)
+      float4 p[RM];
 #pragma unroll
-      for (int c = 0; c < kDC; ++c) vv[c] = *reinterpret_cast<const float4*>(&sm.v[j][tx * 4 + 64 * c]);
+      for (int r = 0; r < RM; ++r) p[r] = *reinterpret_cast<const float4*>(&sm.p[ty * RM + r][j]);
 #pragma unroll
-      for (int r = 0; r < RM; ++r) {
-        const float p = sm.p[ty * RM + r][j];
-        if (edge && __float_as_int(p) < 0) continue;   // hidden: v may be anything
+      for (int e = 0; e < 4; ++e) {
+        float4 vv[kDC];
 #pragma unroll
-        for (int c = 0; c < kDC; ++c) {
-          o[r][c].x = fmaf(p, vv[c].x, o[r][c].x);
-          o[r][c].y = fmaf(p, vv[c].y, o[r][c].y);
-          o[r][c].z = fmaf(p, vv[c].z, o[r][c].z);
-          o[r][c].w = fmaf(p, vv[c].w, o[r][c].w);
+        for (int c = 0; c < kDC; ++c) vv[c] = *reinterpret_cast<const float4*>(&sm.v[j + e][tx * 4 + 64 * c]);
+#pragma unroll
+        for (int r = 0; r < RM; ++r) {
+          const float u = e == 0 ? p[r].x : e == 1 ? p[r].y : e == 2 ? p[r].z : p[r].w;
+          if (edge && __float_as_int(u) < 0) continue; // hidden: v may be anything
+#pragma unroll
+          for (int c = 0; c < kDC; ++c) {
+            o[r][c].x = fmaf(u, vv[c].x, o[r][c].x);
+            o[r][c].y = fmaf(u, vv[c].y, o[r][c].y);
+            o[r][c].z = fmaf(u, vv[c].z, o[r][c].z);
+            o[r][c].w = fmaf(u, vv[c].w, o[r][c].w);
+          }
         }
       }
     }
@@ -466,12 +491,12 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
   }
 }
 
-// Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for two CTAs per SM,
+// Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for `ctas` CTAs per SM,
 // each with at least `least` keys, at most `most` parts (a power of two).
-int splits_for(long long work, int max_tokens, int least, int most) {
+int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2) {
   const int n_sm = sm_count();
   int z = 1;
-  while (z < most && work * z < 2 * n_sm && max_tokens / (2 * z) >= least) z *= 2;
+  while (z < most && work * z < ctas * n_sm && max_tokens / (2 * z) >= least) z *= 2;
   return z;
 }
 
@@ -482,7 +507,7 @@ cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
   cudaError_t e = opt_in(attn_f32_kernel<D, RM>, bytes, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)a.ch.max_rows * a.group + 16 * RM - 1) / (16 * RM);
-  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8);
+  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8, RM == 1 ? 2 : 8);
   return launch_clusters(attn_f32_kernel<D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
                          a.splits, bytes, st, a);
 }
