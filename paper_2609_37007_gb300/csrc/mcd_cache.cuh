@@ -74,9 +74,14 @@ inline mcd_status check_chunks(const mcd_chunks* ch, const mcd_paged_kv* kv) {
 }
 inline bool no_rows(const mcd_chunks* ch) { return ch->n_seqs == 0 || ch->n_rows == 0 || ch->max_rows == 0; }
 
+// SMs of the current device, looked up once per device.
 inline int sm_count() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 152;
-  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return n;
+  const int k = known[dev].load(std::memory_order_relaxed);
+  if (k) return k;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 

@@ -221,21 +221,27 @@ __global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const ForkArgs
   uint8_t* pool = static_cast<uint8_t*>(which ? a.kv.v : a.kv.k);
   const uint8_t* src = pool + (base + from * a.kv.page_stride) * es;
   uint8_t* dst = pool + (base + to * a.kv.page_stride) * es;
-  const int n = a.kv.n_kv_heads * tokens * per;
-  constexpr int kAhead = 4;                            // loads in flight per thread
-  for (int i0 = threadIdx.x; i0 < n; i0 += kAhead * kCopyThreads) {
+  // a thread keeps its 16-byte piece and goes through (head, token) in steps of the CTA's other threads, kAhead loads in
+  // flight; divisions are outside (in the loop they were most of 126 instructions a piece)
+  const int piece = threadIdx.x % per, stride = kCopyThreads / per, dh = stride / tokens, dt = stride % tokens;
+  const long long hs = a.kv.head_stride * es, ts = a.kv.token_stride * es;
+  int h = threadIdx.x / per / tokens, t = threadIdx.x / per % tokens;
+  src += piece * 16;
+  dst += piece * 16;
+  constexpr int kAhead = 4;
+  while (h < a.kv.n_kv_heads) {
     uint4 x[kAhead];
     long long at[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int i = i0 + j * kCopyThreads;
-      const int piece = i % per, rest = i / per, t = rest % tokens, h = rest / tokens;
-      at[j] = (h * a.kv.head_stride + t * a.kv.token_stride) * es + piece * 16;
-      if (i < n) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + at[j]));
+      at[j] = h < a.kv.n_kv_heads ? h * hs + t * ts : -1;
+      if (at[j] >= 0) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + at[j]));
+      h += dh, t += dt;
+      if (t >= tokens) t -= tokens, ++h;
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      if (i0 + j * kCopyThreads < n) *reinterpret_cast<uint4*>(dst + at[j]) = x[j];
+      if (at[j] >= 0) *reinterpret_cast<uint4*>(dst + at[j]) = x[j];
   }
 }
 
@@ -314,24 +320,22 @@ __global__ void __launch_bounds__(kCopyThreads) compact_kernel(const CompactArgs
         }
       }
     } else {
-      const int work = tokens * columns;
-      constexpr int kAhead = 4;
-      for (int i0 = threadIdx.x; i0 < work; i0 += kAhead * kCopyThreads) {
-        uint4 x[kAhead];
-        long long dst[kAhead];
+      // a thread keeps its piece; its tokens one after another, kAhead heads' loads in flight
+      const int piece = threadIdx.x % per;
+      const long long hs = a.kv.head_stride * es;
+      constexpr int kAhead = 8;
+      for (int t = threadIdx.x / per; t < tokens; t += kCopyThreads / per) {
+        const uint8_t* src = pool + from[t] + piece * 16;
+        uint8_t* dst = pool + to[t] + piece * 16;
+        for (int h = 0; h < a.kv.n_kv_heads; h += kAhead, src += kAhead * hs, dst += kAhead * hs) {
+          uint4 x[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const int i = i0 + j * kCopyThreads;
-          const int piece = i % per, rest = i / per, t = rest % tokens, h = rest / tokens;
-          const long long off = h * a.kv.head_stride * es + piece * 16;
-          if (i < work) {
-            x[j] = __ldcs(reinterpret_cast<const uint4*>(pool + from[t] + off));
-            dst[j] = to[t] + off;
-          }
+          for (int j = 0; j < kAhead; ++j)
+            if (h + j < a.kv.n_kv_heads) x[j] = __ldcs(reinterpret_cast<const uint4*>(src + j * hs));
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j)
+            if (h + j < a.kv.n_kv_heads) *reinterpret_cast<uint4*>(dst + j * hs) = x[j];
         }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-          if (i0 + j * kCopyThreads < work) *reinterpret_cast<uint4*>(pool + dst[j]) = x[j];
       }
     }
     __syncthreads();

@@ -19,7 +19,8 @@ namespace paged {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeRows = 8;           // rows of a CTA's tile: one warp looks up each
+constexpr int kRopeRows = 4;           // rows that a CTA's threads hold at a time
+constexpr int kRopeSteps = 2;          // of these, at most, one after another
 
 struct RopeArgs {
   mcd_paged_kv kv;
@@ -31,24 +32,34 @@ struct RopeArgs {
   const float *q_norm, *k_norm;
   int* err;
   long long qkv_stride, q_stride;
-  int layer, n_q;
+  int layer, n_q, steps;
   float eps;
 };
 
+// Eight elements as they lie, and as fp32.
 template <class T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[8]);
+struct Raw8;
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
-  const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = __ldcs(reinterpret_cast<const float4*>(p));
+    b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+};
 template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float (&x)[8]) {
-  const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Raw8<uint16_t> {
+  uint4 a;
+  __device__ __forceinline__ void load(const uint16_t* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo_f32(w[i]), x[2 * i + 1] = bf16_hi_f32(w[i]);
-}
+    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo_f32(w[i]), x[2 * i + 1] = bf16_hi_f32(w[i]);
+  }
+};
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
@@ -58,6 +69,20 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
                                             pack_bf16x2(x[6], x[7]));
 }
 
+__device__ __forceinline__ void load_gain(float (&g)[8], const float* from) {
+  const float4 u = __ldg(reinterpret_cast<const float4*>(from)), v = __ldg(reinterpret_cast<const float4*>(from) + 1);
+  g[0] = u.x, g[1] = u.y, g[2] = u.z, g[3] = u.w, g[4] = v.x, g[5] = v.y, g[6] = v.z, g[7] = v.w;
+}
+// Pairs (x[0], x[1]), (x[2], x[3]), ..
+__device__ __forceinline__ void turn_neighbours(float (&x)[8], const float* cosv, const float* sinv) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float u = x[2 * e], v = x[2 * e + 1];
+    x[2 * e] = u * cosv[e] - v * sinv[e];
+    x[2 * e + 1] = u * sinv[e] + v * cosv[e];
+  }
+}
+
 // Where a row goes: place of head 0 in the layer's pages (elements; -1: the row is nobody's or its
 // sequence does not fit) and its position.
 struct RowPlace {
@@ -65,114 +90,141 @@ struct RowPlace {
   int pos;
 };
 
-// In: type of the qkv rows, Out: type of the cache.  A CTA takes tiles of kRopeRows rows: first a warp
-// per row finds the row's place while the angles' factors are made, then all threads the (row, pair) angles,
-// then eight elements of a head per thread (head_dim / 8 neighbouring lanes hold a head).
+// In: type of the qkv rows, Out: type of the cache.  A CTA takes a.steps times kRopeRows rows: a warp per row finds the
+// rows' places, then every thread makes (row, pair) angles.  For the heads a thread keeps one row and two pieces of
+// eight dimensions, both elements of eight pairs (D / 16 neighbouring lanes hold a head), so that its cosines, sines
+// and gains stay in registers and no element crosses lanes; it goes through the heads in steps of its group,
+// kAhead heads' loads in flight, the first ones before the row's place is known.
+// (A piece and its pairs' other halves by shuffles: 110 instructions for 16 bytes, issue-bound, 60 us where this takes
+// the time below.)
 template <class In, class Out, int D>
-__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArgs a) {
-  constexpr int kLanes = D / 8;                        // lanes of a head
+__global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const RopeArgs a) {
+  constexpr int kLanes = D / 16, kGroups = kRopeThreads / (kLanes * kRopeRows), kAhead = sizeof(In) == 2 ? 4 : 2;
   __shared__ unsigned long long turn[D / 2];           // F_j
-  __shared__ float2 cs[kRopeRows][D / 2];              // (cos, sin) * scale of the tile's rows
-  __shared__ RowPlace place[kRopeRows];
-  const int half = a.rope.rot_dim / 2, n_heads = a.n_q + 2 * a.kv.n_kv_heads;
+  __shared__ float2 cs[kRopeRows * kRopeSteps][D / 2]; // (cos, sin) * scale
+  __shared__ RowPlace place[kRopeRows * kRopeSteps];
+  const int half = a.rope.rot_dim / 2, n_qk = a.n_q + a.kv.n_kv_heads, n_heads = n_qk + a.kv.n_kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int t = threadIdx.x % kLanes, r = threadIdx.x / kLanes % kRopeRows, group = threadIdx.x / (kLanes * kRopeRows);
+  // first dimension of the two pieces; pairs are 8 t .. 8 t + 7 (behind the pairs: what is left, in order)
+  const bool turned = t < half / 8;
+  const int d0 = a.rope.interleaved || !turned ? 16 * t : 8 * t, d1 = a.rope.interleaved || !turned ? d0 + 8 : d0 + half;
+  const int tile = blockIdx.x * (kRopeRows * a.steps);
   tc::pdl_wait();
   tc::pdl_trigger();
+  const int n_rows = min(__ldg(a.ch.row_start + a.ch.n_seqs), a.ch.n_rows);
+  const int rows = min(kRopeRows * a.steps, n_rows - tile);
+  const In* src = static_cast<const In*>(a.qkv) + (tile + (long long)r) * a.qkv_stride;
+  const int per_step = (n_heads + kAhead * kGroups - 1) / (kAhead * kGroups), n_it = per_step * a.steps;
+  Raw8<In> raw[kAhead][2] = {};
+  auto fetch = [&](int i, int step, int h0) {          // head i of the iteration that starts with (step, h0)
+    const int head = h0 + i * kGroups;
+    if (step * kRopeRows + r < rows && head < n_heads) {
+      const In* p = src + step * (kRopeRows * a.qkv_stride) + head * D;
+      raw[i][0].load(p + d0);
+      raw[i][1].load(p + d1);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(i, 0, group);
   if (threadIdx.x < half) {
     const double w = __ldg(a.rope.inv_freq + threadIdx.x) * 0.15915494309189535;   // turns per position
     turn[threadIdx.x] = (unsigned long long)((w - floor(w)) * 18446744073709551616.0);
   }
-  const int last = __ldg(a.ch.row_start + a.ch.n_seqs);
-  const int n_rows = min(last, a.ch.n_rows);
-  for (long long tile = (long long)blockIdx.x * kRopeRows; tile < n_rows; tile += (long long)gridDim.x * kRopeRows) {
-    const int rows = (int)min((long long)kRopeRows, n_rows - tile);
-    if (warp < rows) {
-      const int row = (int)tile + warp;
-      // (empty sequences share their start with the next one: the last of them has the row)
-      const int s = warp_last_le(a.ch.n_seqs, [&](int i) { return (long long)__ldg(a.ch.row_start + i); }, row);
-      const Seq q = load_seq(a.ch, s);
-      RowPlace p{-1, 0};
-      if (q.n > 0 && row >= q.row0 && row - q.row0 < q.n) {
-        const int slot = q.cached + row - q.row0;
-        const int page = __ldg(a.ch.table + (long long)s * a.ch.table_stride + slot / a.kv.page_size);
-        if (page < 0 || page >= a.kv.n_pages) {
-          if (lane == 0) report(a.err, MCD_ERR_INVALID_ARG);
-        } else {
-          p.at = a.layer * a.kv.layer_stride + page * a.kv.page_stride + slot % a.kv.page_size * a.kv.token_stride;
-          p.pos = a.positions ? __ldg(a.positions + row) : slot;
-        }
+  for (int n = warp; n < rows; n += kRopeThreads / 32) {
+    const int row = tile + n;
+    // (empty sequences share their start with the next one: the last of them has the row)
+    const int s = warp_last_le(a.ch.n_seqs, [&](int i) { return (long long)__ldg(a.ch.row_start + i); }, row);
+    const Seq q = load_seq(a.ch, s);
+    RowPlace p{-1, 0};
+    if (q.n > 0 && row >= q.row0 && row - q.row0 < q.n) {
+      const int slot = q.cached + row - q.row0;
+      const int page = __ldg(a.ch.table + (long long)s * a.ch.table_stride + slot / a.kv.page_size);
+      if (page < 0 || page >= a.kv.n_pages) {
+        if (lane == 0) report(a.err, MCD_ERR_INVALID_ARG);
+      } else {
+        p.at = a.layer * a.kv.layer_stride + page * a.kv.page_stride + slot % a.kv.page_size * a.kv.token_stride;
+        p.pos = a.positions ? __ldg(a.positions + row) : slot;
       }
-      if (lane == 0) place[warp] = p;
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * half; i += kRopeThreads) {
-      const int r = i / half, j = i - r * half;
-      const unsigned long long t = (unsigned long long)(long long)place[r].pos * turn[j];
-      float sn, cn;
-      sincospif((float)(int)(t >> 32) * 4.656612873077393e-10f, &sn, &cn);   // half turns in [-1, 1]
-      cs[r][j] = make_float2(cn * a.rope.scale, sn * a.rope.scale);
-    }
-    __syncthreads();
-    const int n_tasks = rows * n_heads * kLanes;
-    for (int t0 = warp * 32; t0 < n_tasks; t0 += kRopeThreads) {
-      const int t = t0 + lane;                         // (the lanes of a head are in or out together)
-      const bool live = t < n_tasks;
-      const int c = t % kLanes, rest = live ? t / kLanes : 0, r = rest / n_heads, head = rest - r * n_heads;
-      const long long at = place[r].at, row = tile + r;
-      float x[8];
-      load8(static_cast<const In*>(a.qkv) + row * a.qkv_stride + (long long)head * D + c * 8, x);
-      const bool is_v = head >= a.n_q + a.kv.n_kv_heads;
-      const float* gain = head < a.n_q ? a.q_norm : a.k_norm;
-      if (a.q_norm || a.k_norm) {
-        float ss = 0.f;
+    if (lane == 0) place[n] = p;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * half; i += kRopeThreads) {
+    const int row = i / half, j = i - row * half;
+    const unsigned long long f = (unsigned long long)(long long)place[row].pos * turn[j];
+    float sn, cn;
+    sincospif((float)(int)(f >> 32) * 4.656612873077393e-10f, &sn, &cn);   // half turns in [-1, 1]
+    cs[row][j] = make_float2(cn * a.rope.scale, sn * a.rope.scale);
+  }
+  __syncthreads();
+  float cosv[8], sinv[8], gain[2][8];
+  const float* held = nullptr;                         // whose gains these are
+  long long at = -1;
+  Out* q_row = nullptr;
+  int step = 0, h0 = group;
+  for (int it = 0; it < n_it; ++it) {
+    if (h0 == group) {                                 // new rows
+      const int row = step * kRopeRows + r;
+      if (step * kRopeRows >= rows) break;             // (the whole CTA)
+      at = row < rows ? place[row].at : -1;
+      q_row = static_cast<Out*>(a.q_out) + (tile + (long long)row) * a.q_stride;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-        for (int m = kLanes / 2; m; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-        if (gain && !is_v) {
-          const float f = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-          float gv[8];
-          load8(gain + c * 8, gv);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = x[e] * f * gv[e];
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float2 w = turned && row < rows ? cs[row][8 * t + e] : make_float2(1.f, 0.f);
+        cosv[e] = w.x;
+        sinv[e] = w.y;
       }
-      if (half) {
-        const int e0 = c * 8;
-        if (a.rope.interleaved) {
-          if (e0 < 2 * half && !is_v) {
+    }
+    const int h_now = h0;
+    h0 += kAhead * kGroups;
+    if (h0 >= per_step * kAhead * kGroups) h0 = group, ++step;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const float2 w = cs[r][(e0 + e) / 2];
-              const float u = x[e], v = x[e + 1];
-              x[e] = u * w.x - v * w.y;
-              x[e + 1] = u * w.y + v * w.x;
-            }
+    for (int i = 0; i < kAhead; ++i) {
+      const int head = h_now + i * kGroups;            // (the same in the whole warp)
+      float x[8], y[8];
+      raw[i][0].get(x);
+      raw[i][1].get(y);
+      if (it + 1 < n_it) fetch(i, step, h0);           // (the next iteration's, on its way during this one)
+      if (head >= n_heads) continue;
+      if (head < n_qk) {
+        const float* norm = head < a.n_q ? a.q_norm : a.k_norm;
+        if (norm) {
+          if (norm != held) {
+            held = norm;
+            load_gain(gain[0], norm + d0);
+            load_gain(gain[1], norm + d1);
           }
-        } else {                                       // the partner's eight elements are half / 8 lanes away
-          const bool low = e0 < half, in = e0 < 2 * half;
-          const int from = in ? lane + (low ? half / 8 : -(half / 8)) : lane;
-          float y[8];
+          float ss = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = __shfl_sync(0xffffffffu, x[e], from);
-          if (in && !is_v) {
+          for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+#pragma unroll
+          for (int m = kLanes / 2; m; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+          const float f = rsqrtf(ss * (1.f / D) + a.eps);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= f * gain[0][e], y[e] *= f * gain[1][e];
+        }
+        if (turned) {
+          if (a.rope.interleaved) {
+            turn_neighbours(x, cosv, sinv);
+            turn_neighbours(y, cosv + 4, sinv + 4);
+          } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float2 w = cs[r][e0 + e - (low ? 0 : half)];
-              x[e] = low ? x[e] * w.x - y[e] * w.y : y[e] * w.y + x[e] * w.x;
+              const float u = x[e], v = y[e];
+              x[e] = u * cosv[e] - v * sinv[e];
+              y[e] = u * sinv[e] + v * cosv[e];
             }
           }
         }
       }
-      if (!live || at < 0) continue;
-      if (head < a.n_q) {
-        store8(static_cast<Out*>(a.q_out) + row * a.q_stride + (long long)head * D + c * 8, x);
-      } else {
-        const int h = head - a.n_q - (is_v ? a.kv.n_kv_heads : 0);
-        store8(static_cast<Out*>(is_v ? a.kv.v : a.kv.k) + at + h * a.kv.head_stride + c * 8, x);
-      }
+      if (at < 0) continue;
+      Out* to = head < a.n_q    ? q_row + head * D
+                : head < n_qk   ? static_cast<Out*>(a.kv.k) + at + (head - a.n_q) * a.kv.head_stride
+                                : static_cast<Out*>(a.kv.v) + at + (head - n_qk) * a.kv.head_stride;
+      store8(to + d0, x);
+      store8(to + d1, y);
     }
-    __syncthreads();                                   // the tile's tables are free again
   }
   if (blockIdx.x == 0)
     for (int s = threadIdx.x; s < a.ch.n_seqs; s += kRopeThreads)
@@ -180,9 +232,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
 }
 
 template <class In, class Out>
-cudaError_t launch_rope(const RopeArgs& a, cudaStream_t st) {
-  const int tiles = (a.ch.n_rows + kRopeRows - 1) / kRopeRows;
-  const dim3 grid(std::min(tiles, sm_count() * 8));
+cudaError_t launch_rope(RopeArgs a, cudaStream_t st) {
+  // as many steps as leave two CTAs (what an SM holds) for every SM
+  a.steps = std::max(1, std::min(kRopeSteps, a.ch.n_rows / (2 * kRopeRows * sm_count())));
+  const dim3 grid((unsigned)(((long long)a.ch.n_rows + kRopeRows * a.steps - 1) / (kRopeRows * a.steps)));
   auto k = a.kv.head_dim == 64 ? rope_append_kernel<In, Out, 64> : rope_append_kernel<In, Out, 128>;
   return tc::launch(true, k, grid, dim3(kRopeThreads), 0, st, a);
 }
@@ -214,7 +267,7 @@ extern "C" mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, con
   if (!aligned16(qkv) || !aligned16(q_out) || qkv_stride * esize(qkv_dtype) % 16 || q_stride * esize(kv->dtype) % 16 ||
       !aligned16(q_norm) || !aligned16(k_norm))
     return MCD_ERR_UNSUPPORTED;
-  const RopeArgs a{*kv, *chunks, *rope, qkv, q_out, positions, q_norm, k_norm, err, qkv_stride, q_stride, layer, n_q_heads, eps};
+  const RopeArgs a{*kv, *chunks, *rope, qkv, q_out, positions, q_norm, k_norm, err, qkv_stride, q_stride, layer, n_q_heads, 1, eps};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32) return cuda_status(launch_rope<float, float>(a, st));
   return cuda_status(qkv_dtype == MCD_WEIGHT_F32 ? launch_rope<float, uint16_t>(a, st) : launch_rope<uint16_t, uint16_t>(a, st));

@@ -330,69 +330,99 @@ def mcd_tc_gemm_tiled(M: int, N: int, K: int, bn: int, A_tiled, B_tiled, Y, err,
 
 
 # ---- paged cache (include/mcd_cache.h) ---------------------------------------------------
+# These calls are short, so that their checks of arguments are too: no helper call per property, descriptors carry
+# their address, torch's types are looked up once.
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
+_F32 = _BF16 = _I32 = _F64 = None
 
 
-def _stream(stream) -> Optional[int]:
-    return stream.cuda_stream if stream is not None else None
+def _types():
+    """torch's types, once a descriptor is built (the module itself does without torch)."""
+    global _F32, _BF16, _I32, _F64
+    if _F32 is None:
+        import torch
+        _F32, _BF16, _I32, _F64 = torch.float32, torch.bfloat16, torch.int32, torch.float64
 
 
 def _kv_dtype(t) -> int:
-    import torch
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("rows and pages are float32 or bfloat16")
-    return 0 if t.dtype == torch.float32 else 1      # MCD_WEIGHT_F32 / MCD_WEIGHT_BF16
+    if t.dtype is _F32:
+        return 0                    # MCD_WEIGHT_F32
+    if t.dtype is _BF16:
+        return 1                    # MCD_WEIGHT_BF16
+    raise ValueError("rows and pages are float32 or bfloat16")
 
 
-def _i32(t, what: str, shape=None):
-    """An int32 device tensor whose rows are read one after another."""
-    import torch
+def _i32(t, what: str, n: int = -1) -> Optional[int]:
+    """Address of a contiguous int32 device tensor (of n elements, where given)."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what}: a contiguous int32 tensor" + ("" if shape is None else f" of shape {tuple(shape)}"))
-    return _ptr(t)
+    if t.dtype is not _I32 or not t.is_contiguous() or not t.is_cuda or (n >= 0 and t.numel() != n):
+        raise ValueError(f"{what}: a contiguous int32 CUDA tensor" + ("" if n < 0 else f" of {n} elements"))
+    return t.data_ptr()
 
 
-def _f32(t, what: str, n: int):
-    import torch
+def _gain(t, n: int) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{what}: {n} contiguous float32 values")
-    return _ptr(t)
+    if t.dtype is not _F32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"norm gains: {n} contiguous float32 values on the device")
+    return t.data_ptr()
+
+
+def _rows(t, what: str, n_rows: int, width: int) -> int:
+    """Row stride (elements) of a packed device row buffer whose rows hold `width` contiguous elements."""
+    n = len(t)
+    if not t.is_cuda:
+        raise ValueError(f"{what}: device buffers must be CUDA tensors")
+    if t.is_contiguous():
+        row = stride = t.numel() // n if n else 0
+    else:
+        row, stride = 1, t.stride(0)
+        for size, st in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            if size != 1 and st != row:
+                raise ValueError(f"{what}: a row's elements are contiguous")
+            row *= size
+    if n < n_rows or row < width:
+        raise ValueError(f"{what}: at least {n_rows} rows of {width} elements")
+    return max(stride, row) if n < 2 else stride
+
+
+def _space(t) -> Tuple[Optional[int], int]:
+    return (None, 0) if t is None else (_ptr(t), t.nbytes)
 
 
 def paged_kv(k, v) -> McdPagedKV:
     """Descriptor of a page pool: k and v device tensors [layers, pages, kv heads, page size, head dim]
     (float32 or bfloat16) of the same shape and strides, the last dimension contiguous.  It keeps them."""
+    _types()
     if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride() or k.stride(4) != 1:
         raise ValueError("k and v: [layers, pages, kv heads, page size, head dim] alike, the last dimension contiguous")
     st = k.stride()
     d = McdPagedKV(_ptr(k), _ptr(v), st[0], st[1], st[2], st[3], *k.shape, _kv_dtype(k))
-    d.kept = (k, v)
+    d.kept, d.addr, d.type = (k, v), ctypes.addressof(d), k.dtype
     return d
 
 
 def chunks(table, cached, row_start, n_rows: int, max_rows: int, max_tokens: int) -> McdChunks:
     """Descriptor of a call's new rows: table int32 [sequences, columns], cached int32 [sequences], row_start
     int32 [sequences + 1], all on the device; the rest are host bounds.  It keeps them."""
+    _types()
     n = cached.numel()
     if table.dim() != 2 or table.shape[0] != n:
         raise ValueError("table: [sequences, columns]")
-    d = McdChunks(_i32(table, "table"), _i32(cached, "cached"), _i32(row_start, "row_start", (n + 1,)), n, table.shape[1], n_rows,
+    d = McdChunks(_i32(table, "table"), _i32(cached, "cached"), _i32(row_start, "row_start", n + 1), n, table.shape[1], n_rows,
                   max_rows, max_tokens)
-    d.kept = (table, cached, row_start)
+    d.kept, d.addr = (table, cached, row_start), ctypes.addressof(d)
     return d
 
 
 def rope(inv_freq=None, rot_dim: int = 0, interleaved: bool = False, scale: float = 1.0) -> McdRope:
     """Descriptor of a rotation: inv_freq float64 [rot_dim / 2] on the device; rot_dim 0: none."""
-    import torch
-    if rot_dim and (inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or inv_freq.numel() != rot_dim // 2):
+    _types()
+    if rot_dim and (inv_freq.dtype is not _F64 or not inv_freq.is_contiguous() or inv_freq.numel() != rot_dim // 2):
         raise ValueError("inv_freq: rot_dim / 2 contiguous float64 values")
     d = McdRope(_ptr(inv_freq) if rot_dim else None, scale, rot_dim, int(interleaved))
-    d.kept = inv_freq
+    d.kept, d.addr = inv_freq, ctypes.addressof(d)
     return d
 
 
@@ -406,34 +436,24 @@ def mcd_rope_freqs(rot_dim: int, base: float, kind: int = ROPE_PLAIN, factor: fl
     return out, float(scale.value)
 
 
-def _rows(t, what: str, n_rows: int, width: int) -> int:
-    """Row stride (elements) of a packed row buffer whose rows hold `width` contiguous elements."""
-    st, row = t.stride(), 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(st[1:])):
-        if size != 1 and stride != row:
-            raise ValueError(f"{what}: a row's elements are contiguous")
-        row *= size
-    if t.shape[0] < n_rows or row < width:
-        raise ValueError(f"{what}: at least {n_rows} rows of {width} elements")
-    return st[0] if t.shape[0] > 1 else row
-
-
 def mcd_rope_append(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: int, qkv, q_out, rot: McdRope, err,
                     positions=None, q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
     """New rows' q | k | v (qkv [rows, (q + 2 kv heads) * head dim]) normalised, rotated, written to q_out
     [rows, q heads * head dim] (the cache's type) and to the pages of `layer`; asynchronous."""
-    d = kv.head_dim
-    if _kv_dtype(q_out) != kv.dtype:
+    d, n = kv.head_dim, ch.n_rows
+    if q_out.dtype is not kv.type:
         raise ValueError("q_out has the cache's type")
-    _check("mcd_rope_append", load_library().mcd_rope_append(
-        ctypes.addressof(kv), layer, ctypes.addressof(ch), n_q_heads, _ptr(qkv),
-        _rows(qkv, "qkv", ch.n_rows, (n_q_heads + 2 * kv.n_kv_heads) * d), _kv_dtype(qkv), _ptr(q_out),
-        _rows(q_out, "q_out", ch.n_rows, n_q_heads * d), ctypes.addressof(rot), _i32(positions, "positions", (ch.n_rows,)),
-        _f32(q_norm, "q_norm", d), _f32(k_norm, "k_norm", d), eps, _i32(err, "err"), _stream(stream)))
+    st = (_lib or load_library()).mcd_rope_append(
+        kv.addr, layer, ch.addr, n_q_heads, qkv.data_ptr(), _rows(qkv, "qkv", n, (n_q_heads + 2 * kv.n_kv_heads) * d), _kv_dtype(qkv),
+        q_out.data_ptr(), _rows(q_out, "q_out", n, n_q_heads * d), rot.addr,
+        None if positions is None else _i32(positions, "positions", n), None if q_norm is None else _gain(q_norm, d),
+        None if k_norm is None else _gain(k_norm, d), eps, _i32(err, "err"), None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_rope_append", st)
 
 
 def mcd_paged_attention_workspace(kv: McdPagedKV, ch: McdChunks, n_q_heads: int) -> int:
-    return int(load_library().mcd_paged_attention_workspace(ctypes.addressof(kv), ctypes.addressof(ch), n_q_heads))
+    return int(load_library().mcd_paged_attention_workspace(kv.addr, ch.addr, n_q_heads))
 
 
 def mcd_paged_attention(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: int, q, out, scale: float, workspace, err,
@@ -441,15 +461,21 @@ def mcd_paged_attention(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: in
     """out [rows, q heads * head dim] = attention of the new rows q over the pages of `layer`, causal, or among the new
     rows as the bits of mask (int32 [rows, words]) say; workspace: uint8, mcd_paged_attention_workspace
     bytes, or None where that is 0.  Asynchronous."""
-    w = n_q_heads * kv.head_dim
-    if _kv_dtype(q) != kv.dtype or _kv_dtype(out) != kv.dtype:
+    w, n = n_q_heads * kv.head_dim, ch.n_rows
+    if q.dtype is not kv.type or out.dtype is not kv.type:
         raise ValueError("q and out have the cache's type")
-    if mask is not None and (mask.dim() != 2 or mask.shape[0] < ch.n_rows):
-        raise ValueError("mask: [rows, words]")
-    _check("mcd_paged_attention", load_library().mcd_paged_attention(
-        ctypes.addressof(kv), layer, ctypes.addressof(ch), n_q_heads, _ptr(q), _rows(q, "q", ch.n_rows, w), _ptr(out),
-        _rows(out, "out", ch.n_rows, w), scale, _i32(mask, "mask"), 0 if mask is None else mask.shape[1], _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(), _i32(err, "err"), _stream(stream)))
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] < n:
+            raise ValueError("mask: [rows, words]")
+        words = mask.shape[1]
+    space, size = _space(workspace)
+    st = (_lib or load_library()).mcd_paged_attention(
+        kv.addr, layer, ch.addr, n_q_heads, q.data_ptr(), _rows(q, "q", n, w), out.data_ptr(), _rows(out, "out", n, w), scale,
+        None if mask is None else _i32(mask, "mask"), words, space, size, _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_paged_attention", st)
 
 
 def mcd_pages_fork_workspace(n_src: int, table_out) -> int:
@@ -461,21 +487,29 @@ def mcd_pages_fork(kv: McdPagedKV, ref_in, ref_out, table_in, len_in, parent, ta
     """Sequences of table_out from those of table_in (int32 device tensors throughout); asynchronous."""
     n_src, src_cols = table_in.shape
     n_dst, dst_cols = table_out.shape
-    _check("mcd_pages_fork", load_library().mcd_pages_fork(
-        ctypes.addressof(kv), _i32(ref_in, "ref_in", (kv.n_pages,)), _i32(ref_out, "ref_out", (kv.n_pages,)), n_src,
-        _i32(table_in, "table_in"), src_cols, _i32(len_in, "len_in", (n_src,)), n_dst, _i32(parent, "parent", (n_dst,)),
-        _i32(reserve, "reserve", (n_dst,)), _i32(table_out, "table_out"), dst_cols, _i32(len_out, "len_out", (n_dst,)), int(release),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _i32(err, "err"), _stream(stream)))
+    n_pages = kv.n_pages
+    space, size = _space(workspace)
+    st = (_lib or load_library()).mcd_pages_fork(
+        kv.addr, _i32(ref_in, "ref_in", n_pages), _i32(ref_out, "ref_out", n_pages), n_src, _i32(table_in, "table_in"), src_cols,
+        _i32(len_in, "len_in", n_src), n_dst, _i32(parent, "parent", n_dst), None if reserve is None else _i32(reserve, "reserve", n_dst),
+        _i32(table_out, "table_out"), dst_cols, _i32(len_out, "len_out", n_dst), int(release), space, size, _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_pages_fork", st)
 
 
 def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, len_out, err, stream=None):
     """Kept tokens of every sequence moved together, in all layers (int32 device tensors throughout; len_out may be
     None); asynchronous."""
     n, cols = table_in.shape
-    _check("mcd_pages_compact", load_library().mcd_pages_compact(
-        ctypes.addressof(kv), n, _i32(table_in, "table_in"), _i32(table_out, "table_out", (n, cols)), cols,
-        _i32(start, "start", (n,)), _i32(keep, "keep", (n, keep.shape[1])), keep.shape[1], _i32(n_keep, "n_keep", (n,)),
-        _i32(len_out, "len_out", (n,)), _i32(err, "err"), _stream(stream)))
+    if keep.dim() != 2 or len(keep) != n:
+        raise ValueError("keep: [sequences, most kept]")
+    st = (_lib or load_library()).mcd_pages_compact(
+        kv.addr, n, _i32(table_in, "table_in"), _i32(table_out, "table_out", n * cols), cols, _i32(start, "start", n), _i32(keep, "keep"),
+        keep.shape[1], _i32(n_keep, "n_keep", n), None if len_out is None else _i32(len_out, "len_out", n), _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_pages_compact", st)
 
 
 def mcd_status_str(status: int) -> str:
