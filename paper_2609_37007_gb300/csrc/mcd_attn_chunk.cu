@@ -192,6 +192,33 @@ __global__ void __launch_bounds__(kCThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr unsigned long long kWait = 2000000000ull;
 
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    mbar_init(q_full, q_boxes ? 1 : 8);
+    mbar_init(drain, 1);
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(&s_full[w], 1);
+      mbar_init(&p_full[2 * w], 4);                    // either half of P
+      mbar_init(&p_full[2 * w + 1], 4);
+      mbar_init(&o_full[w], 1);
+    }
+    for (int i = 0; i < S / 2; ++i) {
+      mbar_init(&v_full[i], 1);
+      mbar_init(&v_seen[i], 1);
+    }
+    *abort_flag = 0;
+    *odd = 0;
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  if (warp == 8 && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+  }
   tc::pdl_wait();
   tc::pdl_trigger();
   // Which tiles: slots of a sequence start at floor(row_start * group / 256) + its number, so that no
@@ -223,28 +250,6 @@ __global__ void __launch_bounds__(kCThreads, 1)
   // for every phase of them, as it could not for the ring's, whose earlier phases it has no part in.
   const int first_look = max(0, (min(keys.hi, q.cached + (a.mask ? 0 : i_first + 1)) - keys.lo) / kCTile);
 
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < S; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
-    }
-    mbar_init(q_full, q_boxes ? 1 : 8);
-    mbar_init(drain, 1);
-    for (int w = 0; w < 2; ++w) {
-      mbar_init(&s_full[w], 1);
-      mbar_init(&p_full[2 * w], 4);                    // either half of P
-      mbar_init(&p_full[2 * w + 1], 4);
-      mbar_init(&o_full[w], 1);
-    }
-    for (int i = 0; i < S / 2; ++i) {
-      mbar_init(&v_full[i], 1);
-      mbar_init(&v_seen[i], 1);
-    }
-    *abort_flag = 0;
-    *odd = 0;
-    fence_barrier_init();
-    fence_proxy_async();
-  }
   if (warp == 9) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -468,25 +473,39 @@ __global__ void __launch_bounds__(kCThreads, 1)
         }
         const uint64_t scale = pack2(a.c, a.c), shift = pack2(-mc, -mc);
         uint64_t sum[2] = {0ull, 0ull};                // (two zeros each)
+        // thirty-two at a time: arguments and exponentials; sums and packing under the next ones' exponentials
+        auto exps = [&](int c) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+          for (int e = 0; e < 32; e += 2) {
+            float u, v;
+            unpack2(fma2(pack2(__uint_as_float(x[c][e]), __uint_as_float(x[c][e + 1])), scale, shift), u, v);
+            x[c][e] = __float_as_uint(u), x[c][e + 1] = __float_as_uint(v);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+r"(x[c][e]));
+        };
+        auto take = [&](int c) {
           uint32_t y[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            float u, v;
-            unpack2(fma2(pack2(__uint_as_float(x[c][2 * e]), __uint_as_float(x[c][2 * e + 1])), scale, shift), u, v);
-            u = ex2(u), v = ex2(v);
+            const float u = __uint_as_float(x[c][2 * e]), v = __uint_as_float(x[c][2 * e + 1]);
             sum[e & 1] = add2(sum[e & 1], pack2(u, v));
             y[e] = pack_bf16x2(u, v);
           }
           tmem_st16(s_col(w) + lanes + 16 * c, y);
-          if (c == 1) {                                // half of P: the product may start
-            tmem_stored();
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[2 * w]);
-          }
-        }
+        };
+        exps(0);
+        exps(1);
+        take(0);
+        take(1);
+        exps(2);
+        tmem_stored();                                 // half of P: the product may start
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[2 * w]);
+        exps(3);
+        take(2);
+        take(3);
         float u, v;
         unpack2(add2(sum[0], sum[1]), u, v);
         l += u + v;
