@@ -230,9 +230,19 @@ __global__ void __launch_bounds__(kSThreads, 3)
     abort_flag = n_issued = 0;
     fence_barrier_init();
     fence_proxy_async();
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
+  // Loads of a tile: a lane per box (`rows` places of a page) and chunk of 64 dimensions, K and V.
+  const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
+  const int rows = min(a.kv.page_size, kSTile), boxes = kSTile / rows;
+  const int my_box = lane / (2 * kDC), my_chunk = lane % kDC;
+  const bool my_v = lane / kDC & 1;
   tc::pdl_wait();
   tc::pdl_trigger();
+  // the first tiles' pages on their way with the lengths (one part only: it starts at key 0)
+  const int first_col = (warp * kSTile + my_box * rows) / a.kv.page_size;
+  const int first_page = a.splits == 1 && warp < S && my_box < boxes && first_col < a.ch.table_stride ? __ldg(table + first_col) : 0;
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && split == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   if (q.n <= 0 || q.n > kSVecs / a.group) return;      // (more: the chunk kernel's)
@@ -242,15 +252,11 @@ __global__ void __launch_bounds__(kSThreads, 3)
   const int n_tiles = (keys.hi - keys.lo + kSTile - 1) / kSTile;
   __syncthreads();                                     // the barriers
 
-  // Tile t into its stage, by one warp: a lane per box (`rows` places of a page) and chunk of 64 dimensions, K and V.
-  const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
-  const int rows = min(a.kv.page_size, kSTile), boxes = kSTile / rows;
-  const int my_box = lane / (2 * kDC), my_chunk = lane % kDC;
-  const bool my_v = lane / kDC & 1;
-  auto load_tile = [&](int t) {
+  // Tile t into its stage, by one warp.
+  auto load_tile = [&](int t, bool first) {
     const int pos = keys.lo + t * kSTile + my_box * rows;
     const bool mine = my_box < boxes && pos < keys.hi;
-    int page = mine ? __ldg(table + pos / a.kv.page_size) : 0;
+    int page = !mine ? 0 : first && a.splits == 1 ? first_page : __ldg(table + pos / a.kv.page_size);
     if (page < 0 || page >= a.kv.n_pages) {
       report(a.err, MCD_ERR_INVALID_ARG);
       page = 0;
@@ -263,7 +269,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
                my_chunk * 64, pos % a.kv.page_size, h, page, &full[t % S]);
     if (lane == 0) atomicMax(&n_issued, t + 1);
   };
-  if (warp < min(S, n_tiles)) load_tile(warp);
+  if (warp < min(S, n_tiles)) load_tile(warp, true);
 
   // the vectors as A fragments: rows lane / 4 and + 8, columns 2 (lane % 4) and + 8 of every 16
   uint4 qf[D / 16];
@@ -406,7 +412,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
       }
     }
     __syncthreads();                                   // the tile has been read: its stage takes tile t + S
-    if (t + S < n_tiles && warp == (t & 3) && !*(volatile int*)&abort_flag) load_tile(t + S);
+    if (t + S < n_tiles && warp == (t & 3) && !*(volatile int*)&abort_flag) load_tile(t + S, false);
   }
   __syncthreads();
   if (abort_flag) {                                    // copies that were late land before their place is used again
