@@ -46,40 +46,48 @@ struct Raw8<float> {
     a = __ldcs(reinterpret_cast<const float4*>(p));
     b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
   }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  __device__ __forceinline__ void get(uint64_t (&x)[4]) const {
+    x[0] = pack2(a.x, a.y), x[1] = pack2(a.z, a.w), x[2] = pack2(b.x, b.y), x[3] = pack2(b.z, b.w);
   }
 };
 template <>
 struct Raw8<uint16_t> {
   uint4 a;
   __device__ __forceinline__ void load(const uint16_t* p) { a = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void get(float (&x)[8]) const {
+  __device__ __forceinline__ void get(uint64_t (&x)[4]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo_f32(w[i]), x[2 * i + 1] = bf16_hi_f32(w[i]);
+    for (int i = 0; i < 4; ++i) x[i] = pack2(bf16_lo_f32(w[i]), bf16_hi_f32(w[i]));
   }
 };
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+__device__ __forceinline__ void store8(float* p, const uint64_t (&x)[4]) {
+  float4 u, v;
+  unpack2(x[0], u.x, u.y), unpack2(x[1], u.z, u.w), unpack2(x[2], v.x, v.y), unpack2(x[3], v.z, v.w);
+  reinterpret_cast<float4*>(p)[0] = u;
+  reinterpret_cast<float4*>(p)[1] = v;
 }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                            pack_bf16x2(x[6], x[7]));
+__device__ __forceinline__ void store8(uint16_t* p, const uint64_t (&x)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float u, v;
+    unpack2(x[i], u, v);
+    w[i] = pack_bf16x2(u, v);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-
-__device__ __forceinline__ void load_gain(float (&g)[8], const float* from) {
+__device__ __forceinline__ void load_gain(uint64_t (&g)[4], const float* from) {
   const float4 u = __ldg(reinterpret_cast<const float4*>(from)), v = __ldg(reinterpret_cast<const float4*>(from) + 1);
-  g[0] = u.x, g[1] = u.y, g[2] = u.z, g[3] = u.w, g[4] = v.x, g[5] = v.y, g[6] = v.z, g[7] = v.w;
+  g[0] = pack2(u.x, u.y), g[1] = pack2(u.z, u.w), g[2] = pack2(v.x, v.y), g[3] = pack2(v.z, v.w);
 }
-// Pairs (x[0], x[1]), (x[2], x[3]), ..
-__device__ __forceinline__ void turn_neighbours(float (&x)[8], const float* cosv, const float* sinv) {
+// Neighbours (x.lo, x.hi), ..: pair e of x by angles (lo or hi of c[e / 2], s[e / 2]).
+__device__ __forceinline__ void turn_neighbours(uint64_t (&x)[4], const uint64_t* c, const uint64_t* s) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float u = x[2 * e], v = x[2 * e + 1];
-    x[2 * e] = u * cosv[e] - v * sinv[e];
-    x[2 * e + 1] = u * sinv[e] + v * cosv[e];
+    float u, v, c0, c1, s0, s1;
+    unpack2(x[e], u, v), unpack2(c[e / 2], c0, c1), unpack2(s[e / 2], s0, s1);
+    const float cc = e % 2 ? c1 : c0, ss = e % 2 ? s1 : s0;
+    x[e] = fma2(pack2(v, u), pack2(-ss, ss), mul2(x[e], pack2(cc, cc)));
   }
 }
 
@@ -158,7 +166,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
     cs[row][j] = make_float2(cn * a.rope.scale, sn * a.rope.scale);
   }
   __syncthreads();
-  float cosv[8], sinv[8], gain[2][8];
+  uint64_t cosv[4], sinv[4], gain[2][4];               // two of each an element
   const float* held = nullptr;                         // whose gains these are
   long long at = -1;
   Out* q_row = nullptr;
@@ -170,10 +178,12 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
       at = row < rows ? place[row].at : -1;
       q_row = static_cast<Out*>(a.q_out) + (tile + (long long)row) * a.q_stride;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float2 w = turned && row < rows ? cs[row][8 * t + e] : make_float2(1.f, 0.f);
-        cosv[e] = w.x;
-        sinv[e] = w.y;
+      for (int e = 0; e < 4; ++e) {
+        const bool there = turned && row < rows;
+        const float2 u = there ? cs[row][8 * t + 2 * e] : make_float2(1.f, 0.f);
+        const float2 v = there ? cs[row][8 * t + 2 * e + 1] : make_float2(1.f, 0.f);
+        cosv[e] = pack2(u.x, v.x);
+        sinv[e] = pack2(u.y, v.y);
       }
     }
     const int h_now = h0;
@@ -182,7 +192,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int head = h_now + i * kGroups;            // (the same in the whole warp)
-      float x[8], y[8];
+      uint64_t x[4], y[4];
       raw[i][0].get(x);
       raw[i][1].get(y);
       if (it + 1 < n_it) fetch(i, step, h0);           // (the next iteration's, on its way during this one)
@@ -195,25 +205,32 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
             load_gain(gain[0], norm + d0);
             load_gain(gain[1], norm + d1);
           }
-          float ss = 0.f;
+          uint64_t squares = mul2(x[0], x[0]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
+          for (int e = 1; e < 4; ++e) squares = fma2(x[e], x[e], squares);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) squares = fma2(y[e], y[e], squares);
+          float ss, odd;
+          unpack2(squares, ss, odd);
+          ss += odd;
 #pragma unroll
           for (int m = kLanes / 2; m; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
           const float f = rsqrtf(ss * (1.f / D) + a.eps);
+          const uint64_t ff = pack2(f, f);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= f * gain[0][e], y[e] *= f * gain[1][e];
+          for (int e = 0; e < 4; ++e) x[e] = mul2(x[e], mul2(ff, gain[0][e])), y[e] = mul2(y[e], mul2(ff, gain[1][e]));
         }
         if (turned) {
           if (a.rope.interleaved) {
             turn_neighbours(x, cosv, sinv);
-            turn_neighbours(y, cosv + 4, sinv + 4);
+            turn_neighbours(y, cosv + 2, sinv + 2);
           } else {
+            const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float u = x[e], v = y[e];
-              x[e] = u * cosv[e] - v * sinv[e];
-              y[e] = u * sinv[e] + v * cosv[e];
+            for (int e = 0; e < 4; ++e) {
+              const uint64_t u = x[e];
+              x[e] = fma2(mul2(y[e], minus), sinv[e], mul2(u, cosv[e]));
+              y[e] = fma2(u, sinv[e], mul2(y[e], cosv[e]));
             }
           }
         }
