@@ -52,8 +52,10 @@ typedef struct {
 /* The new rows of one call.  Sequence s has cached[s] positions in the cache and brings rows
  * row_start[s] .. row_start[s + 1] - 1 (none is allowed) of the packed row buffers; row i of them
  * has position (slot) cached[s] + i, whose page is in the table before the call.  Rows from
- * row_start[n_seqs] on belong to nobody and are neither read nor written.  A sequence that does not
- * fit the bounds below is skipped (MCD_ERR_INVALID_ARG in err). */
+ * row_start[n_seqs] on belong to nobody: they are not written, and what they hold touches nothing.
+ * A sequence that does not fit the bounds below is skipped (MCD_ERR_INVALID_ARG in err); so is, by
+ * mcd_rope_append, a row whose page number is outside the pool, while mcd_paged_attention gives the rows
+ * that read such a page unspecified values. */
 typedef struct {
   const int32_t* table;      /* dev [n_seqs][table_stride]                              */
   const int32_t* cached;     /* dev [n_seqs]                                            */
@@ -160,8 +162,10 @@ int64_t mcd_pages_fork_workspace(int32_t n_src, int32_t n_dst, int32_t dst_cols)
  * moves to position start[s] + i of table_out; len_out[s] (optional) = start[s] + n_keep[s].
  * table_out may be table_in (in place): then keep is strictly ascending in each row.  Otherwise
  * keep may have any order and name a position twice, and no page that the call writes is one that
- * it reads.  keep: dev int32 [n_seqs][max_keep], entries >= 0.  Both tables have table_cols entries a
- * row.  A sequence whose numbers do not fit is left alone (MCD_ERR_INVALID_ARG in err). */
+ * it reads.  Pages that a sequence writes are its own (mcd_pages_fork leaves part-filled pages so).
+ * keep: dev int32 [n_seqs][max_keep], entries >= 0.  Both tables have table_cols entries a row.  A sequence
+ * whose numbers do not fit (MCD_ERR_INVALID_ARG in err) keeps its len_out, and in place its tokens; in
+ * another table some of its tokens may have moved. */
 mcd_status mcd_pages_compact(const mcd_paged_kv* kv, int32_t n_seqs, const int32_t* table_in, const int32_t* table_out,
                              int32_t table_cols, const int32_t* start, const int32_t* keep, int32_t max_keep,
                              const int32_t* n_keep, int32_t* len_out, int32_t* err, void* stream);

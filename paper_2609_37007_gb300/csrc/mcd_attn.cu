@@ -535,6 +535,16 @@ StepPlan plan_step(const mcd_paged_kv& kv, const mcd_chunks& ch) {
   return more > 8 ? StepPlan{more, true} : StepPlan{z, false};
 }
 
+// Which kernels a bf16 call needs: sequences of up to 16 vectors per KV head go to the step kernel, longer ones to the
+// chunk kernel; the bounds tell when there are only the ones or the others.
+struct Route {
+  bool steps, chunks;
+};
+Route route_of(const mcd_chunks& ch, int group) {
+  const bool chunks = (int64_t)ch.max_rows * group > kSVecs;
+  return {!chunks || (int64_t)ch.n_rows < (int64_t)ch.n_seqs * ch.max_rows, chunks};
+}
+
 template <int D>
 cudaError_t launch_step(AttnArgs a, void* workspace, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
@@ -561,7 +571,7 @@ using namespace mcd;
 extern "C" int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads) {
   using namespace paged;
   if (check_kv(kv) != MCD_OK || check_chunks(chunks, kv) != MCD_OK || no_rows(chunks) || n_q_heads <= 0) return 0;
-  if (kv->dtype != MCD_WEIGHT_BF16) return 0;
+  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(*chunks, std::max(1, n_q_heads / kv->n_kv_heads)).steps) return 0;
   const StepPlan p = plan_step(*kv, *chunks);
   return p.in_workspace ? 4ll * kv->n_kv_heads * chunks->n_seqs * p.splits * kSVecs * (kv->head_dim + 4) : 0;
 }
@@ -592,15 +602,12 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
     return cuda_status(kv->head_dim == 64 ? launch_f32<64>(a, st) : launch_f32<128>(a, st));
-  // bf16: sequences of up to 16 vectors per KV head go to the step kernel, longer ones to the chunk kernel;
-  // the bounds tell when there are only the ones or the others
   AttnArgs b = a;
   cudaError_t e = cudaSuccess;
-  const bool chunks_too = (int64_t)chunks->max_rows * a.group > kSVecs;
-  const bool steps_too = !chunks_too || (int64_t)chunks->n_rows < (int64_t)chunks->n_seqs * chunks->max_rows;
-  if (steps_too) e = kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st);
-  if (e == cudaSuccess && chunks_too) {
-    b.least_vecs = steps_too ? kSVecs : 0;
+  const Route r = route_of(*chunks, a.group);
+  if (r.steps) e = kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st);
+  if (e == cudaSuccess && r.chunks) {
+    b.least_vecs = r.steps ? kSVecs : 0;
     e = launch_chunk(b, st);
   }
   return cuda_status(e);

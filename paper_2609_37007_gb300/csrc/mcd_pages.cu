@@ -254,13 +254,13 @@ struct CompactArgs {
 
 constexpr int kTileTokens = 64;
 
-// Whether sequence s's numbers fit (every thread of the CTA calls it).
-__device__ __forceinline__ bool compact_fits(const CompactArgs& a, int s, int start, int n, bool in_place) {
+// Whether sequence s's numbers fit, of its tokens lo .. hi - 1 (every thread of the CTA calls it).
+__device__ __forceinline__ bool compact_fits(const CompactArgs& a, int s, int start, int n, bool in_place, int lo, int hi) {
   const long long span = (long long)a.cols * a.kv.page_size;
   bool ok = start >= 0 && n >= 0 && n <= a.max_keep && start + (long long)n <= span;
   if (ok) {
     const int32_t* keep = a.keep + (long long)s * a.max_keep;
-    for (int i = threadIdx.x; i < n && ok; i += kCopyThreads) {
+    for (int i = lo + threadIdx.x; i < min(hi, n) && ok; i += kCopyThreads) {
       const int k = __ldg(keep + i);
       ok = k >= 0 && start + (long long)k < span && (!in_place || i == 0 || k > __ldg(keep + i - 1));
       if (ok) {
@@ -290,8 +290,10 @@ __global__ void __launch_bounds__(kCopyThreads) compact_kernel(const CompactArgs
   const int first = kInPlace ? 0 : blockIdx.x * kTileTokens;
   const bool lead = blockIdx.x == 0 && blockIdx.y == 0;
   if (!lead && first >= n) return;
-  if (!compact_fits(a, s, start, n, kInPlace)) {
-    if (lead && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
+  // (in place, and for the length, all of the sequence's numbers; a copy looks at its own)
+  const bool all = kInPlace || lead;
+  if (!compact_fits(a, s, start, n, kInPlace, all ? 0 : first, all ? INT_MAX : first + kTileTokens)) {
+    if (threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
     return;
   }
   if (lead && threadIdx.x == 0 && a.len_out) a.len_out[s] = start + n;
@@ -390,7 +392,7 @@ extern "C" mcd_status mcd_pages_compact(const mcd_paged_kv* kv, int32_t n_seqs, 
   if (n_seqs < 0 || table_cols < 0 || max_keep < 0 || !err) return MCD_ERR_INVALID_ARG;
   if (n_seqs == 0) return MCD_OK;
   if (!start || !n_keep || (table_cols && (!table_in || !table_out)) || (max_keep && !keep)) return MCD_ERR_INVALID_ARG;
-  if (n_seqs > 65535 || kv->n_layers > 32767) return MCD_ERR_UNSUPPORTED;
+  if (n_seqs > 65535 || kv->n_layers > 32767 || (int64_t)table_cols * kv->page_size > INT_MAX) return MCD_ERR_UNSUPPORTED;
   const CompactArgs a{*kv, table_in, table_out, start, keep, n_keep, len_out, err, table_cols, max_keep};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool in_place = table_in == table_out;

@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 4;           // rows that a CTA's threads hold at a time
-constexpr int kRopeSteps = 2;          // of these, at most, one after another
+constexpr int kRopeSteps = 4;          // of these, at most, one after another
 
 struct RopeArgs {
   mcd_paged_kv kv;

@@ -382,7 +382,7 @@ def _rows(t, what: str, n_rows: int, width: int) -> int:
             if size != 1 and st != row:
                 raise ValueError(f"{what}: a row's elements are contiguous")
             row *= size
-    if n < n_rows or row < width:
+    if n_rows and (n < n_rows or row < width):
         raise ValueError(f"{what}: at least {n_rows} rows of {width} elements")
     return max(stride, row) if n < 2 else stride
 

@@ -266,11 +266,11 @@ def test_attention_extreme_scores(cache):
 
 
 @pytest.mark.parametrize("cache", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [4, 30])
-def test_hidden_rows_do_not_touch_a_row(cache, rows):
+@pytest.mark.parametrize("rows,cached,h", [(4, 37, 2), (30, 37, 2), (4, 700, 2), (30, 4100, 2), (3, 9000, 1), (200, 61, 2)])
+def test_hidden_rows_do_not_touch_a_row(cache, rows, cached, h):
     """Keys and values of a later new row are NaN or infinite: the rows before it are as without them, it and the
-    rows behind it are not finite."""
-    d, h, hq, page, cached = 64, 2, 4, 16, 37
+    rows behind it are not finite.  With one part of the keys, and with parts joined by a cluster or in the workspace."""
+    d, hq, page = 64, 2 * h, 16
     b = Batch([rows, 1], [cached, 0], page)
     k, v = pool_pair((1, b.n_pages, h, page, d), TYPES[cache])
     q = torch.randn((b.n_buf, hq * d), device=DEV).to(TYPES[cache])
