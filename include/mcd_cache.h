@@ -19,7 +19,8 @@
  *
  * Conventions are those of mcd.h: a status is returned, nothing aborts across the ABI.  Every call
  * is asynchronous on `stream` (a cudaStream_t of the current device, or NULL for the default
- * stream), allocates nothing and can be captured into a graph.  `err` (device int32, zeroed by the
+ * stream), allocates nothing and can be captured into a graph.  Limits: 65,535 sequences, 1,024 KV heads,
+ * fewer than 2^27 rows of a call (MCD_ERR_UNSUPPORTED beyond).  `err` (device int32, zeroed by the
  * caller) receives the first MCD_ERR_* of what only the device can check: lengths, page numbers and
  * parents that do not fit their bounds (MCD_ERR_INVALID_ARG), no free page left (MCD_ERR_OOM), a wait that
  * gave up (MCD_ERR_TIMEOUT).  No memory outside the given bounds is touched then.  Two calls that
@@ -105,8 +106,8 @@ mcd_status mcd_rope_freqs(int32_t kind, int32_t rot_dim, double base, double fac
  *   q_out      dev [n_rows][q_stride] in the cache's type
  *   positions  dev int32 [n_rows], optional: the rows' positions for the rotation (a drafted tree's
  *              rows: their depths'); NULL: their slots
- * Row strides in elements, rows 16-byte aligned.  No two sequences of one call may write to the
- * same place of a page. */
+ * Row strides in elements, rows 16-byte aligned; q_out may not overlap qkv.  No two sequences of one
+ * call may write to the same place of a page. */
 mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads,
                            const void* qkv, int64_t qkv_stride, int32_t qkv_dtype, void* q_out, int64_t q_stride,
                            const mcd_rope* rope, const int32_t* positions, const float* q_norm, const float* k_norm,
@@ -117,7 +118,7 @@ mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, const mcd_chun
  * of the sequence's new rows 0..i, or, with a mask, the rows j whose bit is set: bit j % 32 of word
  * j / 32 of its mask row (a drafted tree: its ancestors and itself).  A row that sees nothing gets
  * zeros.  What a row does not see does not touch it, whatever it holds (infinities and NaN
- * included).
+ * included); what it sees that is not finite makes its result so.
  *   q, out     dev [n_rows][stride] in the cache's type, n_q_heads heads one after another, query
  *              head h reading KV head h / (n_q_heads / n_kv_heads); row strides in elements, rows
  *              16-byte aligned; out may not overlap q

@@ -1,5 +1,9 @@
 // mcd_paged_attention (include/mcd_cache.h): fp32 caches, and bf16 ones with up to 16 query vectors of a
 // KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
+//
+// Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 59 us, 4.5 TB/s; 4 x 2 to 4 rows over up to
+// 120,000: 245 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 85 us for 24 sequences of 1 to 200 rows over up to
+// 600 (4 heads of 64), a quarter of the fp32 rate.
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -540,6 +544,11 @@ StepPlan plan_step(const mcd_paged_kv& kv, const mcd_chunks& ch) {
 struct Route {
   bool steps, chunks;
 };
+// (no sequence has more rows than the buffers)
+mcd_chunks bounded(mcd_chunks ch) {
+  ch.max_rows = std::min(ch.max_rows, ch.n_rows);
+  return ch;
+}
 Route route_of(const mcd_chunks& ch, int group) {
   const bool chunks = (int64_t)ch.max_rows * group > kSVecs;
   return {!chunks || (int64_t)ch.n_rows < (int64_t)ch.n_seqs * ch.max_rows, chunks};
@@ -571,7 +580,7 @@ using namespace mcd;
 extern "C" int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads) {
   using namespace paged;
   if (check_kv(kv) != MCD_OK || check_chunks(chunks, kv) != MCD_OK || no_rows(chunks) || n_q_heads <= 0) return 0;
-  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(*chunks, std::max(1, n_q_heads / kv->n_kv_heads)).steps) return 0;
+  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(bounded(*chunks), std::max(1, n_q_heads / kv->n_kv_heads)).steps) return 0;
   const StepPlan p = plan_step(*kv, *chunks);
   return p.in_workspace ? 4ll * kv->n_kv_heads * chunks->n_seqs * p.splits * kSVecs * (kv->head_dim + 4) : 0;
 }
@@ -585,10 +594,10 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
   if (s != MCD_OK) return s;
   if ((s = check_chunks(chunks, kv)) != MCD_OK) return s;
   if (layer < 0 || layer >= kv->n_layers || n_q_heads <= 0 || n_q_heads % kv->n_kv_heads || !err || !(scale > 0.f) ||
-      !std::isfinite(scale))
+      !std::isfinite(scale * 1.4426950408889634f))
     return MCD_ERR_INVALID_ARG;
   if (mask && (int64_t)mask_words * 32 < chunks->max_rows) return MCD_ERR_INVALID_ARG;
-  if (n_q_heads / kv->n_kv_heads > 16 || (int64_t)chunks->n_rows * 16 > INT32_MAX) return MCD_ERR_UNSUPPORTED;
+  if (n_q_heads / kv->n_kv_heads > 16) return MCD_ERR_UNSUPPORTED;
   if (no_rows(chunks)) return MCD_OK;
   if (!q || !out || q == out) return MCD_ERR_INVALID_ARG;
   const int64_t width = (int64_t)n_q_heads * kv->head_dim;
@@ -597,14 +606,14 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
     return MCD_ERR_UNSUPPORTED;
   const int64_t need = mcd_paged_attention_workspace(kv, chunks, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
-  const AttnArgs a{*kv, *chunks, q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, 0, nullptr,
+  const AttnArgs a{*kv, bounded(*chunks), q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, 0, nullptr,
                    scale * 1.4426950408889634f};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
     return cuda_status(kv->head_dim == 64 ? launch_f32<64>(a, st) : launch_f32<128>(a, st));
   AttnArgs b = a;
   cudaError_t e = cudaSuccess;
-  const Route r = route_of(*chunks, a.group);
+  const Route r = route_of(a.ch, a.group);
   if (r.steps) e = kv->head_dim == 64 ? launch_step<64>(a, workspace, st) : launch_step<128>(a, workspace, st);
   if (e == cudaSuccess && r.chunks) {
     b.least_vecs = r.steps ? kSVecs : 0;

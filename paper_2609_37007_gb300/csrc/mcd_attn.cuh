@@ -74,9 +74,8 @@ __device__ __forceinline__ void store4(uint16_t* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
 }
 
-// Packed vectors p0 + r of a tile (r < 4096): row of the sequence and head of the group without a division each
-// (64-bit divisions in the loads of Q had taken 40,000 cycles a CTA).  floor(t / group) = t ceil(2^16 / group) >> 16
-// for t < 2^16 / group.
+// Packed vectors p0 + r of a tile (r < 4096): row of the sequence and head of the group without a division each:
+// floor(t / group) = t ceil(2^16 / group) >> 16 for t < 2^16 / group.
 struct Pack {
   int row0, head0, inverse, group;
   __device__ __forceinline__ Pack(int p0, int group) : row0(p0 / group), head0(p0 - row0 * group), inverse((65535 + group) / group), group(group) {}

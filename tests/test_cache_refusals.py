@@ -46,7 +46,7 @@ BAD_KV = [(dict(k=None), INVALID), (dict(v=None), INVALID), (dict(n_layers=0), I
           (dict(page_stride=-16384), UNSUPPORTED), (dict(layer_stride=0), UNSUPPORTED), (dict(n_kv_heads=2000), UNSUPPORTED)]
 BAD_CH = [(dict(n_seqs=-1), INVALID), (dict(n_rows=-1), INVALID), (dict(max_rows=-2), INVALID), (dict(max_tokens=-1), INVALID),
           (dict(table=None), INVALID), (dict(cached=None), INVALID), (dict(row_start=None), INVALID),
-          (dict(max_tokens=65), INVALID), (dict(n_seqs=70000), UNSUPPORTED)]
+          (dict(max_tokens=65), INVALID), (dict(n_seqs=70000), UNSUPPORTED), (dict(n_rows=1 << 27), UNSUPPORTED)]
 
 
 def rope_call(mcd, k=None, c=None, layer=0, n_q=16, qkv=P, qkv_stride=32 * 128, dtype=1, q=P, q_stride=16 * 128, rope="", pos=None, qn=None,
@@ -116,7 +116,7 @@ def test_bf16_rows_need_a_bf16_cache(mcd):
 @pytest.mark.parametrize("bad,want", [
     (dict(layer=2), INVALID), (dict(n_q=12), INVALID), (dict(n_q=8 * 17), UNSUPPORTED), (dict(q=None), INVALID), (dict(out=None), INVALID),
     (dict(out=P), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
-    (dict(scale=float("inf")), INVALID), (dict(q_stride=2047), INVALID), (dict(out_stride=2052), UNSUPPORTED), (dict(q=P + 8), UNSUPPORTED),
+    (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID), (dict(q_stride=2047), INVALID), (dict(out_stride=2052), UNSUPPORTED), (dict(q=P + 8), UNSUPPORTED),
     (dict(err=None), INVALID), (dict(mask=P, words=0), INVALID)])
 def test_attention_refusals(mcd, bad, want):
     if bad.get("n_q") == 8 * 17:

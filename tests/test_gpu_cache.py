@@ -292,6 +292,27 @@ def test_hidden_rows_do_not_touch_a_row(cache, rows, cached, h):
         assert not np.isfinite(o[2:rows]).any()
 
 
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [[1, 1, 2], [30, 1, 70]])
+def test_bounds_may_be_loose(cache, rows):
+    """The bounds of the host are bounds only: far larger ones give the same rows (other parts of the keys may)."""
+    d, h, hq, page = 64, 2, 4, 16
+    b = Batch(rows, [40, 700, 0], page)
+    k, v = pool_pair((1, b.n_pages, h, page, d), TYPES[cache])
+    q = torch.randn((b.n_buf, hq * d), device=DEV).to(TYPES[cache])
+    kv, outs = mcd.paged_kv(k, v), []
+    wide = i32(np.concatenate([b.table, np.full((3, 4000), -1)], 1))
+    for ch in (b.ch, mcd.chunks(wide, i32(b.cached), i32(b.start), b.n_buf, 2 ** 30, wide.shape[1] * page)):
+        out, err = torch.zeros_like(q), err_word()
+        space = torch.empty(mcd.mcd_paged_attention_workspace(kv, ch, hq), dtype=torch.uint8, device=DEV)
+        mcd.mcd_paged_attention(kv, 0, ch, hq, q, out, d ** -0.5, space, err)
+        assert err.item() == 0
+        outs.append(np64(out))
+    # either side within its tolerance (see above), for |o| and spread below 4, reach below 10 (64 products of normal
+    # values at scale 1/8) and 771 keys: bf16 2^-8 (4 + 4), fp32 (2 * 74 * 10 + 2 * 771 + 20) u 4
+    assert np.abs(outs[0] - outs[1]).max() <= 2 * (2.0 ** -8 * 8 if cache == "bf16" else 3042 * U * 4)
+
+
 def test_attention_offsets_past_32_bits():
     """A pool whose pages lie further apart than 2^32 bytes."""
     page, d, h = 16, 128, 2
