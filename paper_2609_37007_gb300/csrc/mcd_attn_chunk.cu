@@ -298,20 +298,23 @@ __global__ void __launch_bounds__(kCThreads, 1)
       ok = ok && warp_wait(bar, parity, a.err, abort_flag);
       return ok;
     };
-    auto wait_load = [&](uint32_t i) { return wait(load_bar(i), load_phase(i)); };
-    auto qk = [&](int w, int j) {
-      const uint32_t qa = smem_u32(smem + w * L::kTileBytes), kb = smem_u32(stage(2 * j));
+    // (stages, phases and descriptors are counted along: their arithmetic would stand in the products' way)
+    const uint64_t q_desc[2] = {tc::sw128_desc(smem_u32(smem)), tc::sw128_desc(smem_u32(smem + L::kTileBytes))};
+    const uint64_t k_desc = tc::sw128_desc(smem_u32(smem + L::kRing)), vd0 = v_desc(smem_u32(smem + L::kRing), kChunk);
+    constexpr uint32_t kStageStep = L::kTileBytes >> 4;       // (descriptors count 16 bytes)
+    auto qk = [&](int w, uint32_t at_k) {
+      const uint64_t kd = k_desc + at_k * kStageStep;
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t at = (k >> 2) * kChunk + (k & 3) * 32;
-          tc::umma_bf16(s_col(w), tc::sw128_desc(qa + at), tc::sw128_desc(kb + at), kQk, k > 0);
+          const uint32_t at = ((k >> 2) * kChunk + (k & 3) * 32) >> 4;
+          tc::umma_bf16(s_col(w), q_desc[w] + at, kd + at, kQk, k > 0);
         }
         tc::umma_commit(&s_full[w]);
       }
     };
-    auto pv = [&](int w, int j) {
-      const uint32_t vb = smem_u32(stage(2 * j + 1));
+    auto pv = [&](int w, int j, uint32_t at_v) {
+      const uint64_t vd = vd0 + at_v * kStageStep;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         if (!wait(&p_full[2 * w + half], j & 1)) return;
@@ -319,25 +322,31 @@ __global__ void __launch_bounds__(kCThreads, 1)
         if (elect_one()) {
 #pragma unroll
           for (int k = 4 * half; k < 4 * half + 4; ++k)
-            umma_ts(o_col(w), s_col(w) + 8 * k, v_desc(vb + k * 2048, kChunk), kPv, (j | k) != 0);
+            umma_ts(o_col(w), s_col(w) + 8 * k, vd + k * (2048 >> 4), kPv, (j | k) != 0);
         }
       }
       if (j + 1 == (w ? n_b : n_a) && elect_one()) tc::umma_commit(&o_full[w]);
     };
-    if (n_tiles > 0 && wait(q_full, 0) && wait_load(0)) {
+    if (n_tiles > 0 && wait(q_full, 0) && wait(&full[0], 0)) {
       tc::tc_fence_after();
       if (n_a > 0) qk(0, 0);
       if (n_b > 0) qk(1, 0);
+      uint32_t at_v = 1, phase = 0;                    // K of tile j + 1 is a stage behind V of tile j
       for (int j = 0; j < n_tiles; ++j) {
-        if (j + 1 < n_tiles && !wait_load(2 * j + 2)) break;
-        if (!wait_load(2 * j + 1)) break;
-        if (const int n = j - first_look; n >= 0 && !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) break;
-        if (j < n_a) pv(0, j);
+        const uint32_t at_k = at_v + 1 < S ? at_v + 1 : 0;
+        if (j + 1 < n_tiles && !wait(&full[at_k], at_k ? phase : phase ^ 1)) break;
+        if (const int n = j - first_look; n < 0) {
+          if (!wait(&full[at_v], phase)) break;
+        } else if (!wait(&v_full[n % (S / 2)], n / (S / 2) & 1) || !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) {
+          break;
+        }
+        if (j < n_a) pv(0, j, at_v);
         if (!ok) break;
-        if (j + 1 < n_a) qk(0, j + 1);
-        if (j < n_b) pv(1, j);
+        if (j + 1 < n_a) qk(0, at_k);
+        if (j < n_b) pv(1, j, at_v);
         if (!ok) break;
-        if (j + 1 < n_b) qk(1, j + 1);
+        if (j + 1 < n_b) qk(1, at_k);
+        if ((at_v += 2) >= S) at_v -= S, phase ^= 1;
       }
     }
     if (elect_one()) tc::umma_commit(drain);
