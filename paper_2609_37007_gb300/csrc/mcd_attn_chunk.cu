@@ -28,6 +28,7 @@ namespace {
 constexpr int kCTile = 128;            // keys of a tile, rows of a tile
 constexpr int kCRows = 256;            // packed vectors of a CTA
 constexpr int kCThreads = 352;
+constexpr int kFirst = 6;              // 16-key steps of P's first part: its product runs under the rest of the softmax
 constexpr float kGrowth = 8.f;         // log2 of the growth of a maximum that O is rescaled for
 
 template <int D>
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     mbar_init(drain, 1);
     for (int w = 0; w < 2; ++w) {
       mbar_init(&s_full[w], 1);
-      mbar_init(&p_full[2 * w], 4);                    // either half of P
+      mbar_init(&p_full[2 * w], 4);                    // either part of P
       mbar_init(&p_full[2 * w + 1], 4);
       mbar_init(&o_full[w], 1);
     }
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         tc::tc_fence_after();
         if (elect_one()) {
 #pragma unroll
-          for (int k = 4 * half; k < 4 * half + 4; ++k)
+          for (int k = half ? kFirst : 0; k < (half ? kCTile / 16 : kFirst); ++k)
             umma_ts(o_col(w), s_col(w) + 8 * k, vd + k * (2048 >> 4), kPv, (j | k) != 0);
         }
       }
@@ -486,14 +487,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
         exps(0);
         exps(1);
         take(0);
-        take(1);
         exps(2);
-        tmem_stored();                                 // half of P: the product may start
+        take(1);
+        take(2);
+        tmem_stored();                                 // three quarters of P: the product may start
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[2 * w]);
         exps(3);
-        take(2);
         take(3);
         float u, v;
         unpack2(add2(sum[0], sum[1]), u, v);
