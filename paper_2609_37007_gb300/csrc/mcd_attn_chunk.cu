@@ -29,6 +29,7 @@ constexpr int kCTile = 128;            // keys of a tile, rows of a tile
 constexpr int kCRows = 256;            // packed vectors of a CTA
 constexpr int kCThreads = 352;
 constexpr int kFirst = 6;              // 16-key steps of P's first part: its product runs under the rest of the softmax
+constexpr int kRanked = 128;           // sequences that are ordered by their tokens
 constexpr float kGrowth = 8.f;         // log2 of the growth of a maximum that O is rescaled for
 
 template <int D>
@@ -43,6 +44,7 @@ struct CLayout {
   static constexpr int kBytes = kStat + 2 * kCRows * 4 + 1024;          // + alignment
   static constexpr int kPitch = D + 4;
   static_assert(kCRows * kPitch * 4 <= kBar, "the parts of o take the tiles' place");
+  static_assert((kRanked + 1) * 8 <= 2 * kCRows * 4, "the order of the sequences takes the statistics' place");
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
@@ -153,6 +155,45 @@ __device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, in
   }
 }
 
+// Pairs of tiles of a sequence (few vectors: the step kernel's).
+__device__ __forceinline__ int pairs_of(const AttnArgs& a, const Seq& q) {
+  const int vecs = max(q.n, 0) * a.group;
+  return vecs <= a.least_vecs ? 0 : (vecs + kCRows - 1) / kCRows;
+}
+
+// Sequence of pair `slot` and the pair's number in it (an empty slot: -1, or too large).  The whole block calls it;
+// seen: shared memory of kRanked + 1 entries.
+__device__ __forceinline__ int2 find_pair(const AttnArgs& a, long long slot, int2* seen) {
+  if (a.ch.n_seqs <= kRanked) {
+    // sequences in the order of their tokens, ties in that of their numbers: thread i finds where i's pairs start
+    int2* found = seen + kRanked;
+    const int i = threadIdx.x;
+    int2 mine = make_int2(0, 0);                       // tokens and pairs
+    if (i < a.ch.n_seqs) {
+      const Seq q = load_seq(a.ch, i);
+      mine = make_int2(q.cached + q.n, pairs_of(a, q));
+      seen[i] = mine;
+    }
+    if (i == 0) *found = make_int2(0, -1);
+    __syncthreads();
+    if (mine.y > 0) {
+      long long at = 0;
+      for (int n = 0; n < a.ch.n_seqs; ++n) {
+        const int2 o = seen[n];
+        at += o.x > mine.x || (o.x == mine.x && n < i) ? o.y : 0;
+      }
+      if (at <= slot && slot < at + mine.y) *found = make_int2(i, (int)(slot - at));
+    }
+    __syncthreads();
+    return *found;
+  }
+  // slots of a sequence start at floor(row_start * group / 256) + its number, so that no two overlap; the last slot
+  // may be empty
+  auto first_slot = [&](int i) { return (long long)__ldg(a.ch.row_start + i) * a.group / kCRows + i; };
+  const int s = warp_last_le(a.ch.n_seqs, first_slot, slot);
+  return make_int2(s, (int)max(-1ll, min(slot - first_slot(s), 0x7fffffffll)));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kCThreads, 1)
     attn_chunk_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
@@ -202,21 +243,20 @@ __global__ void __launch_bounds__(kCThreads, 1)
   }
   tc::pdl_wait();
   tc::pdl_trigger();
-  // Which tiles: slots of a sequence start at floor(row_start * group / 256) + its number, so that no
-  // two overlap; the last slot may be empty.  The tiles that see most keys come first.
+  // Which tiles.  The pairs that see most keys come first: CTAs start in the order of their numbers, and a long one that
+  // starts last is waited for alone.
   const int part = blockIdx.x % a.splits, h = blockIdx.x / a.splits % a.kv.n_kv_heads;
   const long long slot = blockIdx.x / a.splits / a.kv.n_kv_heads;
-  auto first_slot = [&](int i) { return (long long)__ldg(a.ch.row_start + i) * a.group / kCRows + i; };
-  const int s = warp_last_le(a.ch.n_seqs, first_slot, slot);
+  const int2 found = find_pair(a, slot, reinterpret_cast<int2*>(sm_m));
+  const int s = __reduce_max_sync(0xffffffffu, found.x), local = __reduce_max_sync(0xffffffffu, found.y);      // (uniform registers)
   const Seq q = load_seq(a.ch, s);
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.ch.n_seqs; i += kCThreads)
       if (load_seq(a.ch, i).n < 0) report(a.err, MCD_ERR_INVALID_ARG);
-  const int vecs = max(q.n, 0) * a.group, n_pairs = (vecs + kCRows - 1) / kCRows;
-  const long long local = slot - first_slot(s);
-  // (all CTAs of a cluster decide alike; few vectors: the step kernel's)
-  if (local < 0 || local >= n_pairs || vecs <= a.least_vecs) return;
-  const int p0 = (n_pairs - 1 - (int)local) * kCRows;
+  const int vecs = max(q.n, 0) * a.group, n_pairs = pairs_of(a, q);
+  // (all CTAs of a cluster decide alike)
+  if (local < 0 || local >= n_pairs) return;
+  const int p0 = (n_pairs - 1 - local) * kCRows;
   const Pack pack(p0, a.group);
   const int i_first = pack.row0, n_vecs = min(kCRows, vecs - p0);
   auto keys_below = [&](int r) {                       // keys that some vector of the pair below r sees
