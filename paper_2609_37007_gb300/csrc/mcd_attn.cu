@@ -1,9 +1,10 @@
 // mcd_paged_attention (include/mcd_cache.h): fp32 caches, and bf16 ones with up to 16 query vectors of a
 // KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
 //
-// Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 59 us, 4.5 TB/s; 4 x 2 to 4 rows over up to
-// 120,000: 245 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 85 us for 24 sequences of 1 to 200 rows over up to
-// 600 (4 heads of 64), a quarter of the fp32 rate.
+// Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 50.7 us, 5.2 TB/s; 4 x 2 to 4 rows over up to
+// 120,000: 247 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 71 us for 24 sequences of 1 to 200 rows over up to
+// 600 (4 heads of 64), a sixth of the fp32 rate: tiles of 64 rows and 64 keys are half empty, and 16 warps an SM (their
+// registers) issue every other cycle (packed products, half the instructions: the same time).
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -25,14 +26,15 @@ struct FSmem {
 };
 
 template <int D, int RM>
-__global__ void __launch_bounds__(kFThreads) attn_f32_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kernel(const AttnArgs a) {
   extern __shared__ __align__(16) uint8_t f_smem[];
   FSmem<D, RM>& sm = *reinterpret_cast<FSmem<D, RM>*>(f_smem);
   constexpr int kBM = 16 * RM, kDC = D / 64;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int h = blockIdx.y, s = blockIdx.z;
+  const int h = blockIdx.y;
   tc::pdl_wait();
   tc::pdl_trigger();
+  const int s = a.ranked ? by_tokens(a.ch, blockIdx.z) : blockIdx.z;
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   const int z = blockIdx.x % a.splits;
@@ -228,7 +230,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
   __shared__ int abort_flag, n_issued;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(s_smem_raw) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = blockIdx.y, s = blockIdx.z, split = blockIdx.x;
+  const int h = blockIdx.y, split = blockIdx.x;
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) mbar_init(&full[i], 1);
     abort_flag = n_issued = 0;
@@ -238,12 +240,13 @@ __global__ void __launch_bounds__(kSThreads, 3)
     asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
   }
   // Loads of a tile: a lane per box (`rows` places of a page) and chunk of 64 dimensions, K and V.
-  const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
   const int rows = min(a.kv.page_size, kSTile), boxes = kSTile / rows;
   const int my_box = lane / (2 * kDC), my_chunk = lane % kDC;
   const bool my_v = lane / kDC & 1;
   tc::pdl_wait();
   tc::pdl_trigger();
+  const int s = a.ranked ? by_tokens(a.ch, blockIdx.z) : blockIdx.z;
+  const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
   // the first tiles' pages on their way with the lengths (one part only: it starts at key 0)
   const int first_col = (warp * kSTile + my_box * rows) / a.kv.page_size;
   const int first_page = a.splits == 1 && warp < S && my_box < boxes && first_col < a.ch.table_stride ? __ldg(table + first_col) : 0;
@@ -502,13 +505,18 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
 }
 
 // Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for `ctas` CTAs per SM,
-// each with at least `least` keys, at most `most` parts (a power of two).
+// each with at least `least` keys, at most `most` parts (a power of two).  The fp32 chunks above
+// take 124, 71 or 78 us with 2, 4 or 8 CTAs per SM.
 int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2) {
   const int n_sm = sm_count();
   int z = 1;
   while (z < most && work * z < ctas * n_sm && max_tokens / (2 * z) >= least) z *= 2;
   return z;
 }
+
+// Whether the order of the sequences matters: CTAs enough that some start when others end.  With it, 128 single rows
+// over 17 to 1,023 keys take 50.7 us, without 59.1; 24 fp32 chunks 71 and 85.
+bool rank(const mcd_chunks& ch, long long ctas) { return ch.n_seqs > 1 && ch.n_seqs <= kRanked && ctas > 2 * sm_count(); }
 
 template <int D, int RM>
 cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
@@ -517,7 +525,8 @@ cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
   cudaError_t e = opt_in(attn_f32_kernel<D, RM>, bytes, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)a.ch.max_rows * a.group + 16 * RM - 1) / (16 * RM);
-  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8, RM == 1 ? 2 : 8);
+  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8, RM == 1 ? 2 : 4);
+  a.ranked = rank(a.ch, tiles * a.kv.n_kv_heads * a.ch.n_seqs * a.splits);
   return launch_clusters(attn_f32_kernel<D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
                          a.splits, bytes, st, a);
 }
@@ -564,6 +573,7 @@ cudaError_t launch_step(AttnArgs a, void* workspace, cudaStream_t st) {
   if (!page_map(&k_map, a.kv, a.kv.k, a.layer, rows) || !page_map(&v_map, a.kv, a.kv.v, a.layer, rows)) return cudaErrorInvalidValue;
   const StepPlan p = plan_step(a.kv, a.ch);
   a.splits = p.splits;
+  a.ranked = rank(a.ch, (long long)a.kv.n_kv_heads * a.ch.n_seqs * p.splits);
   a.part = p.in_workspace ? static_cast<float*>(workspace) : nullptr;
   e = launch_clusters(attn_step_kernel<D>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a, k_map,
                       v_map);
@@ -607,7 +617,7 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
   const int64_t need = mcd_paged_attention_workspace(kv, chunks, n_q_heads);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
   const AttnArgs a{*kv, bounded(*chunks), q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, 0, nullptr,
-                   scale * 1.4426950408889634f};
+                   scale * 1.4426950408889634f, 0};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
     return cuda_status(kv->head_dim == 64 ? launch_f32<64>(a, st) : launch_f32<128>(a, st));

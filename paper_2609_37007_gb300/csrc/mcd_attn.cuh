@@ -31,7 +31,39 @@ struct AttnArgs {
   int least_vecs;          // the chunk kernel takes sequences with more packed vectors than this
   float* part;             // workspace of the parts (null: the CTAs of a cluster join them)
   float c;                 // scale * log2(e)
+  int ranked;              // sequences are taken in the order of their tokens (by_tokens)
 };
+
+// CTAs start in the order of their numbers, and a long one that starts last is waited for alone: the sequences with most
+// tokens come first.
+constexpr int kRanked = 128;           // sequences that are put in order
+
+// The sequence of rank `at`, ties in the order of their numbers.  The whole block calls it, of kRanked threads at least.
+__device__ __forceinline__ int by_tokens(const mcd_chunks& ch, int at) {
+  __shared__ __align__(16) int tokens[kRanked];
+  __shared__ int found;
+  const int i = threadIdx.x;
+  int mine = -1;
+  if (i < kRanked) {
+    if (i < ch.n_seqs) {
+      const Seq q = load_seq(ch, i);
+      mine = q.n > 0 ? q.cached + q.n : 0;
+    }
+    tokens[i] = mine;
+  }
+  __syncthreads();
+  if (i < ch.n_seqs) {
+    int rank = 0;
+    for (int n = 0; n < ch.n_seqs; n += 4) {           // (places behind the last sequence: -1)
+      const int4 o = *reinterpret_cast<const int4*>(tokens + n);
+      rank += (o.x > mine || (o.x == mine && n < i)) + (o.y > mine || (o.y == mine && n + 1 < i)) +
+              (o.z > mine || (o.z == mine && n + 2 < i)) + (o.w > mine || (o.w == mine && n + 3 < i));
+    }
+    if (rank == at) found = i;
+  }
+  __syncthreads();
+  return __reduce_max_sync(0xffffffffu, found);        // (a uniform register)
+}
 
 // Whether packed vectors of row i (of the sequence's new rows) see key `pos`; keys below q.cached are seen by all.
 __device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int pos) {

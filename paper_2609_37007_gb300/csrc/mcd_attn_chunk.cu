@@ -15,8 +15,11 @@
 //                     such a pair of tiles is computed again, key by key)
 // What bounds it: a pair of tiles has 32 products of 64 cycles a key tile (D = 128; 67 measured, back to back), but
 // S to P takes a tile's softmax about 1,700 cycles (exponentials, packing and tensor memory) and its products
-// about 1,400, one after the other, and the other tile fills only part of that: 3,400 cycles a pair, 1.22 PFLOP/s for
-// 11,559 rows over up to 8,500 keys (392 us; 0.64 of what a library product reaches).
+// about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
+// the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
+// up to 8,500 keys (375 us; 0.66 of what a library product reaches).
+// A CTA fills an SM, and takes about 8 us to start and end: the pairs with most keys start first (32 x 65 rows over 200 to
+// 1,500 keys: 47 us, in the sequences' own order 57.6).
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -29,7 +32,6 @@ constexpr int kCTile = 128;            // keys of a tile, rows of a tile
 constexpr int kCRows = 256;            // packed vectors of a CTA
 constexpr int kCThreads = 352;
 constexpr int kFirst = 6;              // 16-key steps of P's first part: its product runs under the rest of the softmax
-constexpr int kRanked = 128;           // sequences that are ordered by their tokens
 constexpr float kGrowth = 8.f;         // log2 of the growth of a maximum that O is rescaled for
 
 template <int D>

@@ -347,6 +347,41 @@ def test_attention_offsets_past_32_bits():
     assert torch.equal(v[0, 2, :, 0], v[0, 1, :, 14]) and err.item() == 0
 
 
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [127, 128, 129])
+@pytest.mark.parametrize("kind", ["single", "chunks", "mixed", "alike"])
+def test_attention_many_sequences(cache, n, kind):
+    """More CTAs than the GPU holds: which sequence a CTA takes depends on the tokens, ties and empty ones among them."""
+    r = np.random.RandomState(n)
+    rows = {"single": r.randint(0, 2, n), "chunks": r.randint(9, 40, n), "mixed": r.randint(0, 2, n) * r.randint(1, 30, n),
+            "alike": np.full(n, 3)}[kind]
+    cached = np.full(n, 50) if kind == "alike" else r.randint(0, 8, n) * r.randint(0, 60, n)
+    check_attention(rows.tolist(), cached.tolist(), hq=12, h=6, cache=cache, seed=n)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 21])
+def test_bad_numbers_among_many_sequences(cache, rows):
+    d, h, hq, page, n = 64, 6, 12, 16, 100
+    r = np.random.RandomState(rows)
+    b = Batch([rows] * n, r.randint(0, 200, n).tolist(), page)
+    k, v = pool_pair((1, b.n_pages, h, page, d), TYPES[cache])
+    q = torch.randn((b.n_buf, hq * d), device=DEV).to(TYPES[cache])
+    kv, outs = mcd.paged_kv(k, v), []
+    bad = b.cached.copy()
+    bad[[7, 50, 99]] = [-1, 2 ** 31 - 1, b.ch.max_tokens]
+    for c in (b.cached, bad):
+        ch = mcd.chunks(i32(b.table), i32(c), i32(b.start), b.n_buf, rows, b.ch.max_tokens)
+        out, err = torch.full_like(q, 5.0), err_word()
+        space = torch.empty(mcd.mcd_paged_attention_workspace(kv, ch, hq), dtype=torch.uint8, device=DEV)
+        mcd.mcd_paged_attention(kv, 0, ch, hq, q, out, d ** -0.5, space, err)
+        assert err.item() == int(c is bad)                # (1: MCD_ERR_INVALID_ARG)
+        outs.append(out)
+    for s in range(n):
+        at = slice(s * rows, (s + 1) * rows)
+        assert torch.equal(outs[1][at], torch.full_like(outs[1][at], 5.0) if s in (7, 50, 99) else outs[0][at])
+
+
 # ---- numbers that do not fit --------------------------------------------------------------------------
 @pytest.mark.parametrize("what", ["cached", "page", "page_minus", "rows", "order", "tokens"])
 @pytest.mark.parametrize("n", [1, 30])
