@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
     }
   };
   fetch(keys.lo);
+  const bool busy = (threadIdx.x >> 5) * 2 * RM < live;      // the warp has rows
   for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
     __syncthreads();                                   // the tile before has been read
 #pragma unroll
@@ -94,6 +95,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
     }
     __syncthreads();
     if (k0 + kFN < keys.hi) fetch(k0 + kFN);
+    if (!busy) continue;
     float sc[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
