@@ -85,7 +85,10 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
     }
   };
   fetch(keys.lo);
-  const bool busy = (threadIdx.x >> 5) * 2 * RM < live;      // the warp has rows
+  // Of the warp's rows (it may have none): all see the keys below `clear`, none sees one from `reach` on.
+  const int first = (threadIdx.x >> 5) * 2 * RM;
+  const int clear = q.cached + (a.mask ? 0 : pack.row(first) + 1);
+  const int reach = first >= live ? 0 : a.mask ? keys.hi : q.cached + pack.row(min(first + 2 * RM, live) - 1) + 1;
   for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
     __syncthreads();                                   // the tile before has been read
 #pragma unroll
@@ -95,7 +98,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
     }
     __syncthreads();
     if (k0 + kFN < keys.hi) fetch(k0 + kFN);
-    if (!busy) continue;
+    if (k0 >= reach) continue;
     float sc[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
@@ -114,7 +117,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
           sc[r][c] = fmaf(qq.x, kk[c].x, fmaf(qq.y, kk[c].y, fmaf(qq.z, kk[c].z, fmaf(qq.w, kk[c].w, sc[r][c]))));
       }
     }
-    const bool edge = k0 + kFN > q.cached;             // some key of the tile may be hidden from some row
+    const bool edge = k0 + kFN > clear;                // some key of the tile may be hidden from some row
 #pragma unroll
     for (int r = 0; r < RM; ++r) {
       const int row = pack.row(ty * RM + r);
