@@ -564,23 +564,33 @@ __global__ void __launch_bounds__(kCThreads, 1)
           for (int e = 0; e < D / 32; ++e) to[e] = (uint16_t)pack_bf16x2(o[e] * f, 0.f);
         }
       } else {
+        // through the place of the tile's Q (its products are done), so that the lanes write rows and not columns: 1.4 us
+        // a CTA otherwise
         const float f = l == 0.f ? 0.f : 1.f / l;
-        uint16_t* to = static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, min(mine, n_vecs - 1), a.out_stride);
+        constexpr int kC = D / 8;                      // 16-byte pieces of a row
+        uint4* rows = reinterpret_cast<uint4*>(smem + w * L::kTileBytes) + (warp & 3) * 32 * kC;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t y[32];
           tmem_ld32(o_col(w) + lanes + c, y);
           tmem_loaded(y);
-          if (mine < n_vecs) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t z[4];
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t z[4];
 #pragma unroll
-              for (int g = 0; g < 4; ++g)
-                z[g] = l == 0.f ? 0u : pack_bf16x2(__uint_as_float(y[e + 2 * g]) * f, __uint_as_float(y[e + 2 * g + 1]) * f);
-              *reinterpret_cast<uint4*>(to + c + e) = make_uint4(z[0], z[1], z[2], z[3]);
-            }
+            for (int g = 0; g < 4; ++g)
+              z[g] = l == 0.f ? 0u : pack_bf16x2(__uint_as_float(y[e + 2 * g]) * f, __uint_as_float(y[e + 2 * g + 1]) * f);
+            rows[lane * kC + ((c + e) / 8 ^ (lane & 7))] = make_uint4(z[0], z[1], z[2], z[3]);
           }
+        }
+        __syncwarp();
+        uint16_t* out = static_cast<uint16_t*>(a.out);
+        const long long at = vec_at<D>(pack, q, h, min(mine, n_vecs - 1), a.out_stride);
+#pragma unroll 4
+        for (int i = 0; i < kC; ++i) {
+          const int r = i * (32 / kC) + lane / kC, piece = lane % kC;
+          const long long to = __shfl_sync(0xffffffffu, at, r);
+          if (base + r < n_vecs) *reinterpret_cast<uint4*>(out + to + piece * 8) = rows[r * kC + (piece ^ (r & 7))];
         }
       }
     }
