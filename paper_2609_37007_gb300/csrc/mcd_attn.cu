@@ -2,7 +2,7 @@
 // KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
 //
 // Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 50.7 us, 5.2 TB/s; 4 x 2 to 4 rows over up to
-// 120,000: 247 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 71 us for 24 sequences of 1 to 200 rows over up to
+// 120,000: 247 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 68.5 us for 24 sequences of 1 to 200 rows over up to
 // 600 (4 heads of 64), a sixth of the fp32 rate: tiles of 64 rows and 64 keys are half empty, and 16 warps an SM (their
 // registers) issue every other cycle (packed products, half the instructions: the same time).
 #include <algorithm>
@@ -520,7 +520,7 @@ int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2
 }
 
 // Whether the order of the sequences matters: CTAs enough that some start when others end.  With it, 128 single rows
-// over 17 to 1,023 keys take 50.7 us, without 59.1; 24 fp32 chunks 71 and 85.
+// over 17 to 1,023 keys take 50.7 us, without 59.1; 24 fp32 chunks 71 and 85 (as they were then).
 bool rank(const mcd_chunks& ch, long long ctas) { return ch.n_seqs > 1 && ch.n_seqs <= kRanked && ctas > 2 * sm_count(); }
 
 template <int D, int RM>

@@ -17,8 +17,9 @@
 // S to P takes a tile's softmax about 1,700 cycles (exponentials, packing and tensor memory) and its products
 // about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
 // the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
-// up to 8,500 keys (375 us; 0.66 of what a library product reaches).
-// A CTA fills an SM, and takes about 8 us to start and end: the pairs with most keys start first (32 x 65 rows over 200 to
+// up to 8,500 keys (370 to 382 us; 0.66 of what a library product reaches).
+// A CTA fills an SM, and takes about 8 us to start and end (2.5 to its place in the lists, 3 to 4 to the first scores, 2 to
+// their P, 1 to 2 to the rows of o written and the next CTA): the pairs with most keys start first (32 x 65 rows over 200 to
 // 1,500 keys: 47 us, in the sequences' own order 57.6).
 #include <algorithm>
 
@@ -243,6 +244,17 @@ __global__ void __launch_bounds__(kCThreads, 1)
     asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
   }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // (before the trigger: a kernel that it lets start may take tensor memory, and keep it until this one is done)
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  auto give_back = [&](uint32_t at) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(512u) : "memory");
+  };
   tc::pdl_wait();
   tc::pdl_trigger();
   // Which tiles.  The pairs that see most keys come first: CTAs start in the order of their numbers, and a long one that
@@ -257,7 +269,10 @@ __global__ void __launch_bounds__(kCThreads, 1)
       if (load_seq(a.ch, i).n < 0) report(a.err, MCD_ERR_INVALID_ARG);
   const int vecs = max(q.n, 0) * a.group, n_pairs = pairs_of(a, q);
   // (all CTAs of a cluster decide alike)
-  if (local < 0 || local >= n_pairs) return;
+  if (local < 0 || local >= n_pairs) {
+    if (warp == 9) give_back(*tmem_slot);
+    return;
+  }
   const int p0 = (n_pairs - 1 - local) * kCRows;
   const Pack pack(p0, a.group);
   const int i_first = pack.row0, n_vecs = min(kCRows, vecs - p0);
@@ -273,13 +288,6 @@ __global__ void __launch_bounds__(kCThreads, 1)
   // for every phase of them, as it could not for the ring's, whose earlier phases it has no part in.
   const int first_look = max(0, (min(keys.hi, q.cached + (a.mask ? 0 : i_first + 1)) - keys.lo) / kCTile);
 
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  tc::tc_fence_before();
-  __syncthreads();
-  tc::tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   auto s_col = [&](int w) { return tmem + 128u * w; };
   auto o_col = [&](int w) { return tmem + 256u + 128u * w; };
@@ -635,7 +643,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
   }
   if (warp == 9) {
     tc::tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    give_back(tmem);
   }
 }
 
