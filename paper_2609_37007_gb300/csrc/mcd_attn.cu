@@ -520,7 +520,8 @@ int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2
 }
 
 // Whether the order of the sequences matters: CTAs enough that some start when others end.  With it, 128 single rows
-// over 17 to 1,023 keys take 50.7 us, without 59.1; 24 fp32 chunks 71 and 85 (as they were then).
+// over 17 to 1,023 keys take 50.7 us, without 59.1 (all of 512 keys: 72 and 70); 24 fp32 chunks 71 and 85 (as they were
+// then).  A vote of the warp for each sequence in place of a thread's walk through all of them: 59.3.
 bool rank(const mcd_chunks& ch, long long ctas) { return ch.n_seqs > 1 && ch.n_seqs <= kRanked && ctas > 2 * sm_count(); }
 
 template <int D, int RM>

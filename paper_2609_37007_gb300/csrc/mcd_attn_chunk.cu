@@ -18,9 +18,9 @@
 // about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
 // the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
 // up to 8,500 keys (370 to 382 us; 0.66 of what a library product reaches).
-// A CTA fills an SM, and takes about 8 us to start and end (2.5 to its place in the lists, 3 to 4 to the first scores, 2 to
+// A CTA fills an SM, and takes about 8 us to start and end (1.5 to its place in the lists, 3 to 4 to the first scores, 2 to
 // their P, 1 to 2 to the rows of o written and the next CTA): the pairs with most keys start first (32 x 65 rows over 200 to
-// 1,500 keys: 47 us, in the sequences' own order 57.6).
+// 1,500 keys: 45.3 us, in the sequences' own order 57.6).
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -167,25 +167,32 @@ __device__ __forceinline__ int pairs_of(const AttnArgs& a, const Seq& q) {
 // Sequence of pair `slot` and the pair's number in it (an empty slot: -1, or too large).  The whole block calls it;
 // seen: shared memory of kRanked + 1 entries.
 __device__ __forceinline__ int2 find_pair(const AttnArgs& a, long long slot, int2* seen) {
-  if (a.ch.n_seqs <= kRanked) {
-    // sequences in the order of their tokens, ties in that of their numbers: thread i finds where i's pairs start
+  if (a.ranked) {
+    // sequences in the order of their tokens, ties in that of their numbers.  Where do i's pairs start?  A warp asks, its
+    // lanes hold the others (a thread that went through them all took 55 ns each).
     int2* found = seen + kRanked;
     const int i = threadIdx.x;
     int2 mine = make_int2(0, 0);                       // tokens and pairs
     if (i < a.ch.n_seqs) {
       const Seq q = load_seq(a.ch, i);
       mine = make_int2(q.cached + q.n, pairs_of(a, q));
-      seen[i] = mine;
     }
+    if (i < kRanked) seen[i] = mine;                   // (behind the last sequence: no pairs)
     if (i == 0) *found = make_int2(0, -1);
     __syncthreads();
-    if (mine.y > 0) {
-      long long at = 0;
-      for (int n = 0; n < a.ch.n_seqs; ++n) {
-        const int2 o = seen[n];
-        at += o.x > mine.x || (o.x == mine.x && n < i) ? o.y : 0;
-      }
-      if (at <= slot && slot < at + mine.y) *found = make_int2(i, (int)(slot - at));
+    constexpr int kE = kRanked / 32;
+    const int lane = i & 31;
+    int2 o[kE];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) o[e] = seen[lane + 32 * e];
+#pragma unroll 4
+    for (int n = i >> 5; n < a.ch.n_seqs; n += kCThreads / 32) {
+      const int2 x = seen[n];
+      int at = 0;                                      // (pairs of all: fewer than 2^31, as CTAs)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) at += o[e].x > x.x || (o[e].x == x.x && lane + 32 * e < n) ? o[e].y : 0;
+      at = __reduce_add_sync(0xffffffffu, at);
+      if (lane == 0 && at <= slot && slot < at + x.y) *found = make_int2(n, (int)(slot - at));
     }
     __syncthreads();
     return *found;
@@ -693,7 +700,11 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   a.splits = 1;
   while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && a.ch.max_tokens / (2 * a.splits) >= 2 * kCTile)
     a.splits *= 2;
-  const long long grid = slots * a.kv.n_kv_heads * a.splits;
+  // Order costs a CTA 25 ns a sequence, and what it saves is the last CTAs' time: worth it for few of either (65 rows over 200
+  // to 1,500 keys each: 32 sequences 56 us, without 68; 128, the 1,024 CTAs of 8 heads, 191 and 173).
+  a.ranked = a.ch.n_seqs <= kRanked && a.ch.n_seqs * pairs * a.kv.n_kv_heads * a.splits <= 256ll * sm_count();
+  // (ordered sequences leave no slots between them)
+  const long long grid = (a.ranked ? pairs : slots) * a.kv.n_kv_heads * a.splits;
   if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   return launch_clusters(attn_chunk_kernel<D>, dim3((unsigned)grid), kCThreads, a.splits, CLayout<D>::kBytes, st, a, k_map, v_map, q_map, q_boxes);
 }
