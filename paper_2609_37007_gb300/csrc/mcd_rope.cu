@@ -108,13 +108,17 @@ struct RowPlace {
 // the time below.)
 template <class In, class Out, int D>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const RopeArgs a) {
-  constexpr int kLanes = D / 16, kGroups = kRopeThreads / (kLanes * kRopeRows), kAhead = sizeof(In) == 2 ? 4 : 2;
+  constexpr int kLanes = D / 16, kGroup = kLanes * kRopeRows, kGroups = kRopeThreads / kGroup, kAhead = sizeof(In) == 2 ? 4 : 2;
   __shared__ unsigned long long turn[D / 2];           // F_j
   __shared__ float2 cs[kRopeRows * kRopeSteps][D / 2]; // (cos, sin) * scale
   __shared__ RowPlace place[kRopeRows * kRopeSteps];
   const int half = a.rope.rot_dim / 2, n_qk = a.n_q + a.kv.n_kv_heads, n_heads = n_qk + a.kv.n_kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int t = threadIdx.x % kLanes, r = threadIdx.x / kLanes % kRopeRows, group = threadIdx.x / (kLanes * kRopeRows);
+  const int t = threadIdx.x % kLanes, r = threadIdx.x / kLanes % kRopeRows, group = threadIdx.x / kGroup;
+  // Lanes of the warp with the same head: a group.  With D = 64 a warp holds two, whose heads may be of different kinds, so
+  // that only one of them takes the norm's sum.
+  static_assert(kGroup == 16 || kGroup == 32, "a group is a warp or half of one");
+  const unsigned same_head = kGroup == 32 ? 0xffffffffu : 0xffffu << (lane & 16);
   // first dimension of the two pieces; pairs are 8 t .. 8 t + 7 (behind the pairs: what is left, in order)
   const bool turned = t < half / 8;
   const int d0 = a.rope.interleaved || !turned ? 16 * t : 8 * t, d1 = a.rope.interleaved || !turned ? d0 + 8 : d0 + half;
@@ -192,7 +196,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
     if (h0 >= per_step * kAhead * kGroups) h0 = group, ++step;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int head = h_now + i * kGroups;            // (the same in the whole warp)
+      const int head = h_now + i * kGroups;            // (the same in the lanes of same_head)
       uint64_t x[4], y[4];
       raw[i][0].get(x);
       raw[i][1].get(y);
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_append_kernel(const Rope
           unpack2(squares, ss, odd);
           ss += odd;
 #pragma unroll
-          for (int m = kLanes / 2; m; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+          for (int m = kLanes / 2; m; m >>= 1) ss += __shfl_xor_sync(same_head, ss, m);
           const float f = rsqrtf(ss * (1.f / D) + a.eps);
           const uint64_t ff = pack2(f, f);
 #pragma unroll
