@@ -160,7 +160,8 @@ mcd_status mcd_pages_fork(const mcd_paged_kv* kv, const int32_t* ref_in, int32_t
 int64_t mcd_pages_fork_workspace(int32_t n_src, int32_t n_dst, int32_t dst_cols);
 
 /* For every sequence s and i < n_keep[s], all layers: the token at position start[s] + keep[s][i] of table_in
- * moves to position start[s] + i of table_out; len_out[s] (optional) = start[s] + n_keep[s].
+ * moves to position start[s] + i of table_out; len_out[s] (optional) = start[s] + n_keep[s].  len_out is an
+ * array of its own: it may not overlap start, n_keep, keep or a table (MCD_ERR_INVALID_ARG).
  * table_out may be table_in (in place): then keep is strictly ascending in each row.  Otherwise
  * keep may have any order and name a position twice, and no page that the call writes is one that
  * it reads.  Pages that a sequence writes are its own (mcd_pages_fork leaves part-filled pages so).

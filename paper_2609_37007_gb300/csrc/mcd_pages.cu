@@ -255,6 +255,12 @@ struct CompactArgs {
 
 constexpr int kTileTokens = 64;
 
+// Whether two device arrays of int32 share an element (an absent one shares none).
+bool overlap(const int32_t* a, int64_t n_a, const int32_t* b, int64_t n_b) {
+  const auto x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + 4 * n_b && y < x + 4 * n_a;
+}
+
 // Whether sequence s's numbers fit, of its tokens lo .. hi - 1 (every thread of the CTA calls it).
 __device__ __forceinline__ bool compact_fits(const CompactArgs& a, int s, int start, int n, bool in_place, int lo, int hi) {
   const long long span = (long long)a.cols * a.kv.page_size;
@@ -396,6 +402,12 @@ extern "C" mcd_status mcd_pages_compact(const mcd_paged_kv* kv, int32_t n_seqs, 
   if (n_seqs < 0 || table_cols < 0 || max_keep < 0 || !err) return MCD_ERR_INVALID_ARG;
   if (n_seqs == 0) return MCD_OK;
   if (!start || !n_keep || (table_cols && (!table_in || !table_out)) || (max_keep && !keep)) return MCD_ERR_INVALID_ARG;
+  // (a sequence's first CTA writes its length, while others may have yet to read where it starts)
+  const int64_t entries = (int64_t)n_seqs * table_cols;
+  if (overlap(len_out, n_seqs, start, n_seqs) || overlap(len_out, n_seqs, n_keep, n_seqs) ||
+      overlap(len_out, n_seqs, keep, (int64_t)n_seqs * max_keep) || overlap(len_out, n_seqs, table_in, entries) ||
+      overlap(len_out, n_seqs, table_out, entries))
+    return MCD_ERR_INVALID_ARG;
   if (n_seqs > 65535 || kv->n_layers > 32767 || (int64_t)table_cols * kv->page_size > INT_MAX) return MCD_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool in_place = table_in == table_out;

@@ -499,8 +499,8 @@ def mcd_pages_fork(kv: McdPagedKV, ref_in, ref_out, table_in, len_in, parent, ta
 
 
 def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, len_out, err, stream=None):
-    """Kept tokens of every sequence moved together, in all layers (int32 device tensors throughout; len_out may be
-    None); asynchronous."""
+    """Kept tokens of every sequence moved together, in all layers (int32 device tensors throughout; len_out: a tensor
+    of its own that overlaps no other, or None); asynchronous."""
     n, cols = table_in.shape
     if keep.dim() != 2 or len(keep) != n:
         raise ValueError("keep: [sequences, most kept]")
