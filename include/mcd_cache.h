@@ -118,7 +118,8 @@ mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, const mcd_chun
  * of the sequence's new rows 0..i, or, with a mask, the rows j whose bit is set: bit j % 32 of word
  * j / 32 of its mask row (a drafted tree: its ancestors and itself).  A row that sees nothing gets
  * zeros.  What a row does not see does not touch it, whatever it holds (infinities and NaN
- * included); what it sees that is not finite makes its result so.
+ * included).  What it sees counts as the formula has it: a score of -inf has weight 0; a score of +inf or
+ * NaN, no score above -inf, or a value that is not finite (0 times it too) makes the row's result not finite.
  *   q, out     dev [n_rows][stride] in the cache's type, n_q_heads heads one after another, query
  *              head h reading KV head h / (n_q_heads / n_kv_heads); row strides in elements, rows
  *              16-byte aligned; out may not overlap q

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
 #pragma unroll
   for (int r = 0; r < RM; ++r) {
     if (ty * RM + r >= live) continue;
-    const float f = l[r] == 0.f ? 0.f : 1.f / l[r];
+    const float f = normaliser(a, q, pack.row(ty * RM + r), l[r]);
 #pragma unroll
     for (int c = 0; c < kDC; ++c)
       store4(static_cast<float*>(a.out) + vec_at<D>(pack, q, h, ty * RM + r, a.out_stride) + tx * 4 + 64 * c,
@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
       x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     }
     if (a.splits == 1) {
-      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      const float f = normaliser(a, q, pack.row(r), sum);
       store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
     } else if (a.part) {
       float* to = a.part + ((pair * a.splits + split) * kSVecs + r) * (D + 4);
@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
       sum = fmaf(f, ml.y, sum);
       x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const float f = normaliser<false>(a, q, pack.row(r), sum);
     store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
 }

@@ -74,6 +74,23 @@ __device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int
   return (__ldg(a.mask + (long long)(q.row0 + i) * a.mask_words + (j >> 5)) >> (j & 31)) & 1u;
 }
 
+// What row i's unnormalised o is multiplied with, l the sum of its weights.  A sum of zero: the row sees nothing and is
+// zeros, or every key that it sees scores -inf (each has weight 0, as beside a finite score) and 0 / 0 is NaN.
+__device__ __forceinline__ float without_weights(const uint32_t* mask_row, int n) {
+  uint32_t any = 0;
+  for (int j = 0; j < n; j += 32) any |= __ldg(mask_row + (j >> 5)) & (n - j >= 32 ? 0xffffffffu : (1u << (n - j)) - 1u);
+  return any ? NAN : 0.f;
+}
+// (behind a call: in line it takes the chunk and step kernels' last registers, 1 % of their time)
+static __device__ __noinline__ float without_weights_call(const uint32_t* mask_row, int n) { return without_weights(mask_row, n); }
+template <bool kCall = true>
+__device__ __forceinline__ float normaliser(const AttnArgs& a, const Seq& q, int i, float l) {
+  if (l != 0.f) return 1.f / l;
+  if (!a.mask || q.cached > 0) return NAN;             // (without a mask it sees itself)
+  const uint32_t* row = a.mask + (long long)(q.row0 + i) * a.mask_words;
+  return kCall ? without_weights_call(row, q.n) : without_weights(row, q.n);
+}
+
 // Place (elements) of position pos of KV head h in the layer's pages; -1 for a page outside the pool.
 __device__ __forceinline__ long long key_at(const AttnArgs& a, int s, int h, int pos) {
   const int page = __ldg(a.ch.table + (long long)s * a.ch.table_stride + pos / a.kv.page_size);
@@ -161,7 +178,7 @@ __device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int 
 
 // Joins the parts of `vecs` packed vectors that the CTAs of a cluster hold in the same places of their shared
 // memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
-// m = -inf and l = 0; nothing at all gives zeros.
+// m = -inf and l = 0.
 template <class T, int D>
 __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, const Pack& pack, int vecs, float* o, int pitch,
                                              float* m, float* l) {
@@ -182,7 +199,7 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, in
       sum = fmaf(w, *cl.map_shared_rank(l + r, z), sum);
       x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const float f = normaliser(a, q, pack.row(r), sum);
     store4(static_cast<T*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
   cl.sync();                                           // nobody leaves while others read

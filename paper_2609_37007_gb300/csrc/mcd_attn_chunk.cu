@@ -574,14 +574,14 @@ __global__ void __launch_bounds__(kCThreads, 1)
           if (base + r >= n_vecs) break;
           float sl, sm, o[D / 32];
           slow_row<D>(a, q, s, h, pack, base + r, keys, sm, sl, o);
-          const float f = sl == 0.f ? 0.f : 1.f / sl;
+          const float f = normaliser(a, q, pack.row(base + r), sl);
           uint16_t* to = static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, base + r, a.out_stride) + lane * (D / 32);
           for (int e = 0; e < D / 32; ++e) to[e] = (uint16_t)pack_bf16x2(o[e] * f, 0.f);
         }
       } else {
         // through the place of the tile's Q (its products are done), so that the lanes write rows and not columns: 1.4 us
         // a CTA otherwise
-        const float f = l == 0.f ? 0.f : 1.f / l;
+        const float f = normaliser(a, q, row, l);
         constexpr int kC = D / 8;                      // 16-byte pieces of a row
         uint4* rows = reinterpret_cast<uint4*>(smem + w * L::kTileBytes) + (warp & 3) * 32 * kC;
 #pragma unroll 1
@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
             uint32_t z[4];
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-              z[g] = l == 0.f ? 0u : pack_bf16x2(__uint_as_float(y[e + 2 * g]) * f, __uint_as_float(y[e + 2 * g + 1]) * f);
+              z[g] = pack_bf16x2(__uint_as_float(y[e + 2 * g]) * f, __uint_as_float(y[e + 2 * g + 1]) * f);
             rows[lane * kC + ((c + e) / 8 ^ (lane & 7))] = make_uint4(z[0], z[1], z[2], z[3]);
           }
         }
@@ -636,9 +636,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
             tmem_loaded(y);
           }
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)              // (a row that has seen nothing has no o)
+          for (int e = 0; e < 32; e += 4)              // (a row that sees none of the part's keys: P and o are zeros)
             *reinterpret_cast<uint4*>(os + r * L::kPitch + c + e) =
-                some && m > -INFINITY ? make_uint4(y[e], y[e + 1], y[e + 2], y[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
+                some ? make_uint4(y[e], y[e + 1], y[e + 2], y[e + 3]) : make_uint4(0u, 0u, 0u, 0u);
         }
         sm_m[r] = some ? m : -INFINITY;
         sm_l[r] = some ? l : 0.f;
