@@ -6,7 +6,8 @@ import torch
 
 from oracle import paged
 from paper_2609_37007_gb300 import mcd
-from test_gpu_cache import DEV, HALF, TYPES, U, Batch, check_rope, err_word, np64, pool_pair
+from test_gpu_cache import (DEV, HALF, TYPES, U, Batch, check_attention, check_rope, documents, err_word, nothing_sometimes, np64,
+                            pool_pair, tree)
 
 pytestmark = pytest.mark.gpu
 
@@ -126,3 +127,74 @@ def test_masked_rows_without_a_finite_score(cache, rows):
     value = np64(v)[0, b.table[0, 0], 0, 2]
     assert np.isnan(got[[1, last]]).all() and (got[2].reshape(hq, d) == value).all()
     assert (got[[i for i in range(rows) if i not in (1, 2, last)]] == 0).all() and np.isfinite(got[rows:]).all()
+
+
+# ---- attention: precision and head layouts -------------------------------------------------------
+def tolerance(ref, spread, reach, keys, d, p_bits):
+    """Of a bf16 result, as in test_gpu_cache.py but for the probabilities: a relative error of 2^-p_bits."""
+    return 2.0 ** -8 * np.abs(ref) + (2 * ((d + 10) * U * reach + 8 * U) + (2 * keys + 4) * U + 2.0 ** -p_bits) * spread
+
+
+@pytest.mark.parametrize("hq,h,d,rows", [(16, 8, 128, [1, 8, 0, 3]), (4, 4, 64, [16, 1, 9, 2]), (7, 1, 128, [1, 2, 2, 1]), (16, 1, 64, [1, 1, 0, 1]),
+                                         (6, 2, 128, [5, 1, 4, 2])])
+@pytest.mark.parametrize("cached", [[0, 40, 3, 300], [700, 90, 1100, 65], [2500, 2400, 3000, 2600]])
+@pytest.mark.parametrize("mask", [None, tree, nothing_sometimes])
+def test_few_rows_keep_probabilities_of_16_bits(hq, h, d, rows, cached, mask):
+    """Up to 16 query vectors of a KV head multiply probabilities as hi + lo pairs of bf16: hi is off by 2^-8 of a
+    probability at most, lo by 2^-8 of that.  (Of one bf16 alone the results would not pass: test_cache_tolerance.py.)"""
+    b = Batch(rows, cached, 32, seed=hq)
+    k, v = pool_pair((1, b.n_pages, h, 32, d), torch.bfloat16, seed=hq)
+    q = (1.5 * torch.randn((b.n_buf, hq * d), generator=torch.Generator(device=DEV).manual_seed(d), device=DEV)).bfloat16()
+    r = np.random.RandomState(hq)
+    mats = None if mask is None else [mask(r, n) for n in rows]
+    got, qq, kk, vv = run_attention(b, k, v, q, hq, d, mats), np64(q), np64(k), np64(v)
+    for s, n in enumerate(rows):
+        L, lo = n + cached[s], b.start[s]
+        ref, spread, reach = paged.attention(qq[lo:lo + n].reshape(n, hq, d), paged.tokens(kk, 0, b.table[s], L), paged.tokens(vv, 0, b.table[s], L),
+                                             cached[s], d ** -0.5, None if mats is None else mats[s])
+        assert (np.abs(got[lo:lo + n].reshape(n, hq, d) - ref) <= tolerance(ref, spread, reach, L, d, 16)).all()
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [3, 5, 6, 7, 16])
+@pytest.mark.parametrize("mask", [None, documents])
+def test_attention_chunks_of_wide_groups(cache, group, mask):
+    """head_dim 128 and groups that do not divide a tile of 128 vectors, or whose heads fill it with 8 rows."""
+    check_attention([40, 6, 0, 1, 130], [20, 0, 4, 60, 129], hq=2 * group, h=2, d=128, cache=cache, mask=mask, seed=group, poison=True)
+    check_attention([17, 60], [700, 2500], hq=group, h=1, d=128, cache=cache, mask=mask, seed=group, page=64)
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("group,rows", [(1, 17), (1, 127), (1, 128), (1, 129), (1, 130), (2, 64), (2, 65), (3, 43), (16, 8), (16, 9)])
+@pytest.mark.parametrize("cached", [0, 100, 2100])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_hidden_infinities_around_a_tile(cache, group, rows, cached, bad):
+    """Rows that fill a tile of 128 vectors but for one, exactly, or by one more; new rows whose keys and values are not finite,
+    seen by nobody or by themselves alone, beside rows that see nothing at all where nothing is cached."""
+    d, h, page = 128, 1, 32
+    hq, r = group * h, np.random.RandomState(rows)
+    b = Batch([rows, 1], [cached, 3], page, seed=rows)
+    k, v = pool_pair((1, b.n_pages, h, page, d), TYPES[cache], seed=rows)
+    q = torch.randn((b.n_buf, hq * d), generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV).to(TYPES[cache])
+    m = r.randint(0, 2, (rows, rows)).astype(np.uint8)
+    odd = [1, rows // 2, rows - 1]
+    m[:, odd] = 0
+    m[odd[0], odd[0]] = m[odd[2], odd[2]] = 1
+    m[2] = 0
+    for j in odd:
+        t = cached + j
+        for x in (k, v):
+            x[0, b.table[0, t // page], :, t % page] = bad
+    got, qq, kk, vv = run_attention(b, k, v, q, hq, d, [m, np.ones((1, 1), dtype=np.uint8)]), np64(q), np64(k), np64(v)
+    for s, n in enumerate(b.rows):
+        L, lo = n + b.cached[s], b.start[s]
+        with np.errstate(invalid="ignore"):
+            ref, spread, reach = paged.attention(qq[lo:lo + n].reshape(n, hq, d), paged.tokens(kk, 0, b.table[s], L),
+                                                 paged.tokens(vv, 0, b.table[s], L), int(b.cached[s]), d ** -0.5, m if s == 0 else None)
+        o = got[lo:lo + n].reshape(n, hq, d)
+        seers = [odd[0], odd[2]] if s == 0 else []
+        rest = [i for i in range(n) if i not in seers]
+        assert not np.isfinite(o[seers]).any() and np.isfinite(ref[rest]).all()
+        p_error = 2.0 ** -8 if cache == "bf16" else 0.0
+        tol = HALF[cache] * np.abs(ref) + (2 * ((d + 10) * U * reach + 8 * U) + (2 * L + 4) * U + p_error) * spread
+        assert (np.abs(o - ref)[rest] <= tol[rest]).all()
