@@ -198,3 +198,17 @@ def test_hidden_infinities_around_a_tile(cache, group, rows, cached, bad):
         p_error = 2.0 ** -8 if cache == "bf16" else 0.0
         tol = HALF[cache] * np.abs(ref) + (2 * ((d + 10) * U * reach + 8 * U) + (2 * L + 4) * U + p_error) * spread
         assert (np.abs(o - ref)[rest] <= tol[rest]).all()
+
+
+@pytest.mark.parametrize("cache", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cached", [([1], [630]), ([3, 1, 2], [70, 900, 5000]), ([1], [9000]), ([65] * 5, [300, 17, 0, 900, 128]), ([40], [4100]),
+                                         ([1, 30, 300], [50, 0, 700])])
+def test_attention_repeats_itself(cache, rows, cached):
+    """No sum depends on which CTA comes first: the same call gives the same bits."""
+    d, hq, h = 128, 4, 2
+    b = Batch(rows, cached, 64, seed=len(rows))
+    k, v = pool_pair((1, b.n_pages, h, 64, d), TYPES[cache], seed=1)
+    q = torch.randn((b.n_buf, hq * d), device=DEV).to(TYPES[cache])
+    first = run_attention(b, k, v, q, hq, d)
+    for _ in range(4):
+        assert (run_attention(b, k, v, q, hq, d) == first).all()
