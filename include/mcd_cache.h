@@ -1,8 +1,9 @@
 /* libmcd: a paged KV cache of many utterances and the operators around it.
  *
  * mcd_outer (mcd_pipeline.h) decodes one utterance over a cache of its own.  A program that serves
- * many utterances of a Sec. 1 / Fig. 1 model (arXiv 2609.37007) builds its layers from the products
- * of mcd_tc.h and these operators:
+ * many utterances of a Sec. 1 / Fig. 1 model (arXiv 2609.37007) has its layers' cache and attention
+ * from these operators and their products from mcd_tc.h; row norms, activations and residual sums between
+ * them are its own:
  *
  *   mcd_rope_append       the rows of the QKV product: per-head RMSNorm, rotary positions, K and V
  *                         into the cache's pages
@@ -54,9 +55,13 @@ typedef struct {
  * row_start[s] .. row_start[s + 1] - 1 (none is allowed) of the packed row buffers; row i of them
  * has position (slot) cached[s] + i, whose page is in the table before the call.  Rows from
  * row_start[n_seqs] on belong to nobody: they are not written, and what they hold touches nothing.
- * A sequence that does not fit the bounds below is skipped (MCD_ERR_INVALID_ARG in err); so is, by
- * mcd_rope_append, a row whose page number is outside the pool, while mcd_paged_attention gives the rows
- * that read such a page unspecified values. */
+ * A sequence that does not fit the bounds below is skipped (MCD_ERR_INVALID_ARG in err; where row_start is
+ * not ascending, others may be too); so is, by mcd_rope_append, a row whose page number is outside the
+ * pool, while mcd_paged_attention gives the rows that read such a page unspecified values.
+ * Any bounds that hold give the same rows (but for the rounding of sums taken in other parts); the launch
+ * goes by them, so that tight ones are faster.  One bf16 row over 630 keys: 7.6 us, with a max_tokens of
+ * 32,768 20 (as many parts as that would want).  128 single rows: 50.5 us, with a max_rows of 128 64 in bf16
+ * (both kernels are launched) and 445 for 205 in fp32 (a CTA for every tile that there could be). */
 typedef struct {
   const int32_t* table;      /* dev [n_seqs][table_stride]                              */
   const int32_t* cached;     /* dev [n_seqs]                                            */
@@ -106,7 +111,8 @@ mcd_status mcd_rope_freqs(int32_t kind, int32_t rot_dim, double base, double fac
  *   q_out      dev [n_rows][q_stride] in the cache's type
  *   positions  dev int32 [n_rows], optional: the rows' positions for the rotation (a drafted tree's
  *              rows: their depths'); NULL: their slots
- * Row strides in elements, rows 16-byte aligned; q_out may not overlap qkv.  No two sequences of one
+ * Row strides in elements, rows and gains 16-byte aligned, n_q_heads at most 4,096 (MCD_ERR_UNSUPPORTED
+ * otherwise); q_out may not overlap qkv.  No two sequences of one
  * call may write to the same place of a page. */
 mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads,
                            const void* qkv, int64_t qkv_stride, int32_t qkv_dtype, void* q_out, int64_t q_stride,
@@ -128,8 +134,10 @@ mcd_status mcd_rope_append(const mcd_paged_kv* kv, int32_t layer, const mcd_chun
  *   workspace  dev, 16-byte aligned, at least mcd_paged_attention_workspace bytes (a function of the
  *              sizes alone; may be 0: then NULL will do); needs no initial value
  * n_q_heads is a multiple of n_kv_heads, at most 16 times as many.  Scores, softmax statistics and
- * sums are fp32; bf16 models multiply bf16 queries, keys, values and (chunks beyond 16 query vectors per
- * KV head) probabilities on the tensor cores. */
+ * sums are fp32; bf16 models multiply bf16 queries, keys, values and probabilities on the tensor cores: a
+ * sequence with up to 16 query vectors per KV head (its rows times the heads of a group) has probabilities
+ * of two bf16 terms, off by 2^-16, one with more of one term, off by 2^-8; so has every sequence of a call
+ * whose n_rows has room for max_rows of each, if those are more than 16 vectors. */
 mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads,
                                const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
                                const uint32_t* mask, int32_t mask_words, void* workspace, int64_t workspace_bytes,
@@ -144,7 +152,7 @@ int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* 
  *                 parent's first child (lowest d) takes over those that nobody else holds.
  *   ref_out       = ref_in, one more for every entry of table_out, with `release` one less for
  *                 every entry of table_in: the old sequences end.  A page is free while its count
- *                 is 0.
+ *                 is 0: ref_in has 1 at least for every page that a table names.
  * Fresh pages are the free pages of ref_in in ascending order, handed out in the order of d, then of
  * position; what this call releases is free for the next.  With parent = 0, 1, 2, .. and `release` the call
  * only makes room for `reserve` more tokens.  table_in [n_src][src_cols] holds pages for len_in[s]
@@ -168,7 +176,8 @@ int64_t mcd_pages_fork_workspace(int32_t n_src, int32_t n_dst, int32_t dst_cols)
  * it reads.  Pages that a sequence writes are its own (mcd_pages_fork leaves part-filled pages so).
  * keep: dev int32 [n_seqs][max_keep], entries >= 0.  Both tables have table_cols entries a row.  A sequence
  * whose numbers do not fit (MCD_ERR_INVALID_ARG in err) keeps its len_out, and in place its tokens; in
- * another table some of its tokens may have moved. */
+ * another table some of its tokens may have moved.  At most 32,767 layers and table_cols * page_size below 2^31
+ * (MCD_ERR_UNSUPPORTED otherwise). */
 mcd_status mcd_pages_compact(const mcd_paged_kv* kv, int32_t n_seqs, const int32_t* table_in, const int32_t* table_out,
                              int32_t table_cols, const int32_t* start, const int32_t* keep, int32_t max_keep,
                              const int32_t* n_keep, int32_t* len_out, int32_t* err, void* stream);

@@ -3,7 +3,7 @@
 //
 // Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 50.7 us, 5.2 TB/s; 4 x 2 to 4 rows over up to
 // 120,000: 247 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 68.5 us for 24 sequences of 1 to 200 rows over up to
-// 600 (4 heads of 64), a sixth of the fp32 rate: tiles of 64 rows and 64 keys are half empty, and 16 warps an SM (their
+// 600 (4 heads of 64), a sixth of the fp32 rate (128 fp32 single rows over 17 to 1,023: 205 us, 2.6 TB/s): tiles of 64 rows and 64 keys are half empty, and 16 warps an SM (their
 // registers) issue every other cycle (packed products, half the instructions: the same time).
 #include <algorithm>
 
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
 
 // Parts of the keys when `work` (tile, KV head) pairs alone would leave SMs idle: enough for `ctas` CTAs per SM,
 // each with at least `least` keys, at most `most` parts (a power of two).  The fp32 chunks above
-// take 124, 71 or 78 us with 2, 4 or 8 CTAs per SM.
+// took 124, 71 or 78 us with 2, 4 or 8 CTAs per SM.
 int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2) {
   const int n_sm = sm_count();
   int z = 1;
@@ -520,8 +520,9 @@ int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2
 }
 
 // Whether the order of the sequences matters: CTAs enough that some start when others end.  With it, 128 single rows
-// over 17 to 1,023 keys take 50.7 us, without 59.1 (all of 512 keys: 72 and 70); 24 fp32 chunks 71 and 85 (as they were
-// then).  A vote of the warp for each sequence in place of a thread's walk through all of them: 59.3.
+// over 17 to 1,023 keys take 50.5 us, without 59.3 (all of 512 keys: 56.0 and 53.7); 24 fp32 chunks 68.8 and 86.0; 128
+// fp32 single rows 205 and 255.  It takes a thread per sequence, and the step kernel has kRanked: 129 single rows keep the
+// order in which they are given, 59.1.
 bool rank(const mcd_chunks& ch, long long ctas) { return ch.n_seqs > 1 && ch.n_seqs <= kRanked && ctas > 2 * sm_count(); }
 
 template <int D, int RM>

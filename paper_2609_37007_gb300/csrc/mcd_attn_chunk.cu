@@ -17,10 +17,17 @@
 // S to P takes a tile's softmax about 1,700 cycles (exponentials, packing and tensor memory) and its products
 // about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
 // the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
-// up to 8,500 keys (370 to 382 us; 0.66 of what a library product reaches).
+// up to 8,500 keys (370 to 382 us; 0.66 of what a library product reaches; tensor pipe 55 % active).
 // A CTA fills an SM, and takes about 8 us to start and end (1.5 to its place in the lists, 3 to 4 to the first scores, 2 to
 // their P, 1 to 2 to the rows of o written and the next CTA): the pairs with most keys start first (32 x 65 rows over 200 to
-// 1,500 keys: 45.3 us, in the sequences' own order 57.6).
+// 1,500 keys: 45.4 us, in the sequences' own order 59).
+// P is rounded to one bf16, off by 2^-8 of a probability at most, and l sums it unrounded: a hi + lo pair, as the step
+// kernel multiplies, would double the second product, half of the tensor work.  Relative to the norm of the result the
+// error is 2.2e-3 for those trees and 2.3e-3 for the long prompts; the rounding of the result alone gives 1.7e-3.
+// The steps are published ones: running maximum and sum (Milakov and Gimelshein 2018, arXiv 1805.02867), tiles with an
+// unnormalised o (Dao et al. 2022, arXiv 2205.14135), the softmax of one tile under the products of another (Shah et al.
+// 2024, arXiv 2407.08608).  That o is rescaled only where the maximum has grown far, and that P is handed over in
+// parts, are known ideas of recent attention kernels for these tensor cores.
 #include <algorithm>
 
 #include "mcd_attn.cuh"
@@ -701,7 +708,7 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && a.ch.max_tokens / (2 * a.splits) >= 2 * kCTile)
     a.splits *= 2;
   // Order costs a CTA 25 ns a sequence, and what it saves is the last CTAs' time: worth it for few of either (65 rows over 200
-  // to 1,500 keys each: 32 sequences 56 us, without 68; 128, the 1,024 CTAs of 8 heads, 191 and 173).
+  // to 1,500 keys each: 32 sequences 45.4 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
   a.ranked = a.ch.n_seqs <= kRanked && a.ch.n_seqs * pairs * a.kv.n_kv_heads * a.splits <= 256ll * sm_count();
   // (ordered sequences leave no slots between them)
   const long long grid = (a.ranked ? pairs : slots) * a.kv.n_kv_heads * a.splits;

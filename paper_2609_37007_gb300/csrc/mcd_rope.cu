@@ -4,13 +4,14 @@
 // The mathematics: per head x -> x * gain / sqrt(mean x^2 + eps) (queries and keys, optional), then
 // pair j turned by t = position * inv_freq[j]: (a, b) -> scale * (a cos t - b sin t, a sin t + b cos t).
 // The angle is kept in turns as a 64-bit fixed-point fraction, F_j = frac(inv_freq[j] / 2 pi) * 2^64:
-// position * F_j wraps at one turn by itself, so the reduction modulo 2 pi is exact at every
-// position and costs one integer product; what is left of it (32 bits, 2^-33 turns) goes to
-// sincospif.  A double product and its reduction would be bound by the GB300's few fp64 units.
+// position * F_j wraps at one turn by itself, so the reduction modulo one turn is exact at every
+// position and costs one integer product.  The upper 32 bits of what is left go to sincospif as a float of
+// half turns, whose 24 bits round them by up to 2^-26 turns (9e-8 radians), as any fp32 angle up to half a turn
+// is.  A double product and its reduction would be bound by the GB300's few fp64 units.
 //
 // What bounds it: one read of the rows, one write of q and of the pages (HBM); for a few rows the
-// chain row_start -> cached -> table -> store.  12,129 bf16 rows of 32 heads: 52.5 us, 4.1 TB/s (44 without norm and
-// rotation; a copy of as many bytes takes 37).
+// chain row_start -> cached -> table -> store.  13,290 bf16 rows of 32 heads: 52.5 us, 4.1 TB/s (43 without norm and
+// rotation; a copy of as many bytes takes 35); fp32 rows into an fp32 cache 80 us, 5.4 TB/s (a copy: 67).
 #include <algorithm>
 
 #include "mcd_cache.cuh"
