@@ -49,6 +49,19 @@ mcd_status mcd_tc_tile(int32_t R, int32_t K, int32_t ld, const uint16_t* src, vo
 mcd_status mcd_tc_gemm_tiled(int32_t M, int32_t N, int32_t K, int32_t bn, const void* A_tiled, const void* B_tiled,
                              float* Y, int32_t* err, void* stream);
 
+/* Y[n][m] = a_scale[m] * b_scale[n] * sum_k A[m][k] * B[n][k] for m < M, n < N: 8-bit operands (e4m3, the type and the row
+ * scales of mcd_norm_rows), products and sums as with bf16 in fp32, one rounding to Y.
+ *   A        dev [M][lda] (weights), B dev [N][ldb] (rows), K bytes used of each row
+ *   a_scale  dev float [M], b_scale dev float [N]; NULL: ones
+ *   Y        dev [N][ldy], y_dtype MCD_WEIGHT_F32 or MCD_WEIGHT_BF16
+ *   err      dev int32, zeroed by the caller: MCD_ERR_TIMEOUT if a device-side wait gave up
+ * Any sizes up to 2^24; strides in elements, rows 16-byte aligned (MCD_ERR_UNSUPPORTED otherwise).  Y overlaps nothing else.
+ * Few rows of B share the GPU by parts of K, joined in a fixed order; rows do not depend on each other's values, but their last
+ * bit may on N.  Asynchronous on `stream`: no allocation, no workspace, no synchronisation; can be captured. */
+mcd_status mcd_tc_gemm_e4m3(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const float* a_scale,
+                            const void* B, int64_t ldb, const float* b_scale, void* Y, int64_t ldy, int32_t y_dtype,
+                            int32_t* err, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -241,6 +241,12 @@ cudaError_t opt_in(K* kernel, int bytes, std::atomic<unsigned>& done) {
   return e;
 }
 
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// The driver's encoder, looked up once (null: no driver).
+EncodeTiled tensor_map_encoder();
+
 // Tensor map of one layer's pages for tma_page, boxes of `rows` places (false: no driver).
 bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int layer, int rows);
 

@@ -661,26 +661,9 @@ __global__ void __launch_bounds__(kCThreads, 1)
   }
 }
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-// The driver's encoder, looked up once (null: no driver).
-EncodeTiled encoder() {
-  static std::atomic<void*> found{nullptr};
-  void* fn = found.load(std::memory_order_acquire);
-  if (!fn) {
-    cudaDriverEntryPointQueryResult got;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got) != cudaSuccess ||
-        got != cudaDriverEntryPointSuccess)
-      return nullptr;
-    found.store(fn, std::memory_order_release);
-  }
-  return reinterpret_cast<EncodeTiled>(fn);
-}
-
 // Rows of Q, boxes of a tile.
 bool rows_map(CUtensorMap* map, const AttnArgs& a) {
-  const EncodeTiled encode = encoder();
+  const EncodeTiled encode = tensor_map_encoder();
   if (!encode) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)a.kv.head_dim, (cuuint64_t)a.kv.n_kv_heads * a.group, (cuuint64_t)a.ch.n_rows};
   const cuuint64_t strides[2] = {(cuuint64_t)a.kv.head_dim * 2, (cuuint64_t)a.q_stride * 2};
@@ -718,8 +701,21 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
 
 }  // namespace
 
+EncodeTiled tensor_map_encoder() {
+  static std::atomic<void*> found{nullptr};
+  void* fn = found.load(std::memory_order_acquire);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult got;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+        got != cudaDriverEntryPointSuccess)
+      return nullptr;
+    found.store(fn, std::memory_order_release);
+  }
+  return reinterpret_cast<EncodeTiled>(fn);
+}
+
 bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int layer, int rows) {
-  const EncodeTiled encode = encoder();
+  const EncodeTiled encode = tensor_map_encoder();
   if (!encode) return false;
   void* base = static_cast<uint8_t*>(const_cast<void*>(pool)) + layer * kv.layer_stride * 2;
   const cuuint64_t dims[4] = {(cuuint64_t)kv.head_dim, (cuuint64_t)kv.page_size, (cuuint64_t)kv.n_kv_heads, (cuuint64_t)kv.n_pages};

@@ -142,6 +142,9 @@ def load_library() -> ctypes.CDLL:
         "mcd_tc_gemm": (I32, [I32, I32, I32, I32, P, P, P, P]),
         "mcd_tc_tile": (I32, [I32, I32, I32, P, P, P]),
         "mcd_tc_gemm_tiled": (I32, [I32, I32, I32, I32, P, P, P, P, P]),
+        "mcd_tc_gemm_e4m3": (I32, [I32, I32, I32, P, I64, P, P, I64, P, P, I64, I32, P, P]),
+        "mcd_norm_rows": (I32, [I32, I32, P, I64, I32, P, I64, P, I64, I32, I32, P, ctypes.c_float, P, I64, I32, P, P]),
+        "mcd_sample_rows": (I32, [I32, I32, P, I64, I32, P, P, P, P, P, P, P, P, P, P]),
         "mcd_rope_freqs": (I32, [I32, I32, ctypes.c_double, ctypes.c_double, I32, ctypes.c_double, ctypes.c_double,
                                  P, P]),
         "mcd_rope_append": (I32, [P, I32, P, I32, P, I64, I32, P, I64, P, P, P, P, ctypes.c_float, P, P]),
@@ -335,15 +338,15 @@ def mcd_tc_gemm_tiled(M: int, N: int, K: int, bn: int, A_tiled, B_tiled, Y, err,
 # stay (lengths are read on the device): attention of one row over 630 keys takes 7.3 us a call then, 15.3 with a chunks
 # descriptor, its workspace query and the workspace made anew for each.
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
-_F32 = _BF16 = _I32 = _F64 = None
+_F32 = _BF16 = _I32 = _F64 = _E4M3 = None
 
 
 def _types():
     """torch's types, once a descriptor is built (the module itself does without torch)."""
-    global _F32, _BF16, _I32, _F64
+    global _F32, _BF16, _I32, _F64, _E4M3
     if _F32 is None:
         import torch
-        _F32, _BF16, _I32, _F64 = torch.float32, torch.bfloat16, torch.int32, torch.float64
+        _F32, _BF16, _I32, _F64, _E4M3 = torch.float32, torch.bfloat16, torch.int32, torch.float64, torch.float8_e4m3fn
 
 
 def _kv_dtype(t) -> int:
@@ -512,6 +515,80 @@ def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, 
         None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_pages_compact", st)
+
+
+# ---- rows between the products (include/mcd_rows.h) and 8-bit products (include/mcd_tc.h) ----
+def _row_dtype(t) -> int:
+    if t.dtype is _E4M3:
+        return 3                    # MCD_E4M3
+    return _kv_dtype(t)
+
+
+def _per_row(t, dtype, what: str, n: int) -> Optional[int]:
+    """Address of n contiguous device values of a type (None: none)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: {n} contiguous {dtype} values on the device")
+    return t.data_ptr()
+
+
+def _matrix(t, what: str) -> Tuple[int, int]:
+    if t.dim() != 2:
+        raise ValueError(f"{what}: [rows, elements]")
+    return t.shape
+
+
+def mcd_norm_rows(x, y, residual=None, sum_out=None, gain=None, eps: float = 1e-6, norm: bool = True, y_scale=None, stream=None):
+    """y [rows, width] = RMSNorm of x + residual times gain (norm False: without the norm), float32, bfloat16 or float8_e4m3fn
+    with a float32 scale per row in y_scale; the sum goes to sum_out.  x, residual and sum_out float32 or bfloat16.  Asynchronous."""
+    _types()
+    n, w = _matrix(x, "x")
+    if _matrix(y, "y") != (n, w):
+        raise ValueError("y has x's shape")
+    kept = residual if sum_out is None else sum_out
+    if residual is not None and sum_out is not None and residual.dtype is not sum_out.dtype:
+        raise ValueError("residual and sum_out have one type")
+    y_dtype = _row_dtype(y)
+    if y_dtype == 3 and y_scale is None:
+        raise ValueError("8-bit rows need y_scale")
+    st = (_lib or load_library()).mcd_norm_rows(
+        n, w, x.data_ptr(), _rows(x, "x", n, w), _kv_dtype(x), None if residual is None else residual.data_ptr(),
+        0 if residual is None else _rows(residual, "residual", n, w), None if sum_out is None else sum_out.data_ptr(),
+        0 if sum_out is None else _rows(sum_out, "sum_out", n, w), 0 if kept is None else _kv_dtype(kept), int(norm),
+        None if gain is None else _gain(gain, w), eps, y.data_ptr(), _rows(y, "y", n, w), y_dtype, _per_row(y_scale, _F32, "y_scale", n),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_norm_rows", st)
+
+
+def mcd_sample_rows(logits, u, ids, err, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, kept=None, stream=None):
+    """ids int32 [rows]: one id of every row of logits (float32 or bfloat16 [rows, vocab]), drawn with u float64 [rows].  Settings
+    per row: temperature, top_p, min_p float32, top_k int32; probs float32 and kept int32 are optional outputs.  Asynchronous."""
+    _types()
+    n, v = _matrix(logits, "logits")
+    st = (_lib or load_library()).mcd_sample_rows(
+        n, v, logits.data_ptr(), _rows(logits, "logits", n, v), _kv_dtype(logits), _per_row(temperature, _F32, "temperature", n),
+        _per_row(top_k, _I32, "top_k", n), _per_row(top_p, _F32, "top_p", n), _per_row(min_p, _F32, "min_p", n), _per_row(u, _F64, "u", n),
+        _per_row(ids, _I32, "ids", n), _per_row(probs, _F32, "probs", n), _per_row(kept, _I32, "kept", n), _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_sample_rows", st)
+
+
+def mcd_tc_gemm_e4m3(a, b, y, err, a_scale=None, b_scale=None, stream=None):
+    """y [N, M] (float32 or bfloat16) = b a^T of float8_e4m3fn weights a [M, K] and rows b [N, K], times float32 scales per row
+    of a and of b.  Asynchronous."""
+    _types()
+    (m, k), (n, kb) = _matrix(a, "a"), _matrix(b, "b")
+    if a.dtype is not _E4M3 or b.dtype is not _E4M3 or k != kb or _matrix(y, "y") != (n, m):
+        raise ValueError("a [M, K] and b [N, K] are float8_e4m3fn, y is [N, M]")
+    st = (_lib or load_library()).mcd_tc_gemm_e4m3(
+        m, n, k, a.data_ptr(), _rows(a, "a", m, k), _per_row(a_scale, _F32, "a_scale", m), b.data_ptr(), _rows(b, "b", n, k),
+        _per_row(b_scale, _F32, "b_scale", n), y.data_ptr(), _rows(y, "y", n, m), _kv_dtype(y), _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_tc_gemm_e4m3", st)
 
 
 def mcd_status_str(status: int) -> str:
