@@ -2,13 +2,15 @@
  *
  * mcd_outer (mcd_pipeline.h) decodes one utterance over a cache of its own.  A program that serves
  * many utterances of a Sec. 1 / Fig. 1 model (arXiv 2609.37007) has its layers' cache and attention
- * from these operators and their products from mcd_tc.h; row norms, activations and residual sums between
- * them are its own:
+ * from these operators, their products from mcd_tc.h, and the row norms, residual sums and sampled tokens between them
+ * from mcd_rows.h; activations are its own:
  *
  *   mcd_rope_append       the rows of the QKV product: per-head RMSNorm, rotary positions, K and V
  *                         into the cache's pages
  *   mcd_paged_attention   attention of every utterance's new rows over its pages: a single row, a
  *                         few drafted rows, a drafted tree (Fig. 2) or a whole prompt
+ *   mcd_paged_attention_window   the same with a sliding window and a few first positions that stay visible, so that
+ *                         an utterance of any length needs a bounded number of pages
  *   mcd_pages_fork        reorder, duplicate, extend and release utterances by reference counts
  *   mcd_pages_compact     move the kept tokens of every utterance together (accepted tree nodes,
  *                         positions kept when others are dropped)
@@ -143,6 +145,22 @@ mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer, const mcd_
                                const uint32_t* mask, int32_t mask_words, void* workspace, int64_t workspace_bytes,
                                int32_t* err, void* stream);
 int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads);
+
+/* mcd_paged_attention for utterances that remember their last `window` positions and their first n_sinks ones: of what
+ * a row at position p sees there (cached positions and, without a mask, new rows), it keeps the positions j with
+ * p - j < window or j < n_sinks.  p is the row's slot; with a mask it is cached[s] + the number of new rows that it sees - 1
+ * (a drafted tree: the depth's position; a row that sees no new row: cached[s]), and which new rows it sees the mask alone says.
+ * Positions from n_sinks to cached[s] - window are seen by no row: entries of the table whose pages hold nothing else are not
+ * looked at and may be -1, the pages given back.  (mcd_pages_fork and mcd_pages_compact want every page of a sequence in its
+ * row of the table.)
+ *   window     >= 1 (one of max_tokens or more hides nothing), n_sinks >= 0: MCD_ERR_INVALID_ARG otherwise
+ * All else as there, the workspace at least mcd_paged_attention_window_workspace bytes. */
+mcd_status mcd_paged_attention_window(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads,
+                                      const void* q, int64_t q_stride, void* out, int64_t out_stride, float scale,
+                                      int32_t window, int32_t n_sinks, const uint32_t* mask, int32_t mask_words,
+                                      void* workspace, int64_t workspace_bytes, int32_t* err, void* stream);
+int64_t mcd_paged_attention_window_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads,
+                                             int32_t window, int32_t n_sinks);
 
 /* n_dst new sequences from n_src old ones.  Sequence d continues parent[d] (-1: starts empty):
  *   len_out[d]    = the parent's length

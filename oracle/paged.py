@@ -66,6 +66,37 @@ def attention(q: np.ndarray, k: np.ndarray, v: np.ndarray, cached: int, scale: f
     return out, spread, reach
 
 
+def seen_in_window(n: int, cached: int, window: int, sinks: int, mask: Optional[np.ndarray] = None) -> np.ndarray:
+    """[n, cached + n]: which positions each of a sequence's new rows sees."""
+    see = np.zeros((n, cached + n), dtype=bool)
+    for i in range(n):
+        p = cached + i if mask is None else cached + max(1, int(np.asarray(mask[i]).astype(bool).sum())) - 1
+        for j in range(cached + n):
+            near = p - j < window or j < sinks
+            if j < cached:
+                see[i, j] = near
+            else:
+                see[i, j] = bool(mask[i, j - cached]) if mask is not None else j <= p and near
+    return see
+
+
+def attention_seen(q: np.ndarray, k: np.ndarray, v: np.ndarray, see: np.ndarray, scale: float):
+    """attention() of rows that see the positions of see [n, keys]; what nobody sees is not looked at."""
+    n, hq, d = q.shape
+    group = hq // k.shape[1]
+    out, spread, reach = np.zeros((n, hq, d)), np.zeros((n, hq, d)), np.zeros((n, hq, 1))
+    for i in range(n):
+        at = np.flatnonzero(see[i])
+        for h in range(hq if len(at) else 0):
+            kk, vv = k[at, h // group], v[at, h // group]
+            z = scale * (kk @ q[i, h])
+            p = np.exp(z - z.max())
+            p /= p.sum()
+            out[i, h], spread[i, h] = p @ vv, p @ np.abs(vv)
+            reach[i, h] = scale * (np.abs(kk) @ np.abs(q[i, h])).max()
+    return out, spread, reach
+
+
 def fork(ref, table, lens, parent, reserve, cols: int, page: int, release: bool):
     """(ref_out, table_out, len_out, copies) or an error's name; copies: (from page, to page, tokens)."""
     ref = list(ref)

@@ -25,7 +25,7 @@ struct FSmem {
   float q[16 * RM][D + 4], k[kFN][D + 4], v[kFN][D], p[16 * RM][kFN + 4], m[16 * RM], l[16 * RM];
 };
 
-template <int D, int RM>
+template <int D, int RM, bool kWin>
 __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kernel(const AttnArgs a) {
   extern __shared__ __align__(16) uint8_t f_smem[];
   FSmem<D, RM>& sm = *reinterpret_cast<FSmem<D, RM>*>(f_smem);
@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
   const int h = blockIdx.y;
   tc::pdl_wait();
   tc::pdl_trigger();
-  const int s = a.ranked ? by_tokens(a.ch, blockIdx.z) : blockIdx.z;
+  const int s = a.ranked ? by_tokens<kWin>(a, blockIdx.z) : blockIdx.z;
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && blockIdx.x == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   const int z = blockIdx.x % a.splits;
@@ -43,7 +43,9 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
   if (p0 >= vecs) return;                              // (all CTAs of the cluster alike)
   const Pack pack(p0, a.group);
   const int live = min(kBM, vecs - p0), last_row = pack.row(live - 1);
-  const Span keys = part_of(a.mask ? q.cached + q.n : q.cached + last_row + 1, z, a.splits, kFN);
+  const Lows lows = window_lows<kWin>(a, q, pack.row0, last_row);
+  const Gap gap = gap_of<kWin>(a, lows.from, kFN);
+  const Span keys = part_of((a.mask ? q.cached + q.n : q.cached + last_row + 1) - gap.gap, z, a.splits, kFN);
 
   {
     float4 x[RM * D / 64];                             // all loads in flight
@@ -76,8 +78,8 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       kn[i] = vn[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      const int pos = k0 + my_row + i * kStep;
-      const long long at = pos < keys.hi ? key_at(a, s, h, pos) : -1;
+      const int v = k0 + my_row + i * kStep, pos = kWin ? gap.at(k0) + my_row + i * kStep : v;
+      const long long at = v < keys.hi && touched<kWin>(a, lows.from, pos, 1) ? key_at(a, s, h, pos) : -1;
       if (at >= 0) {
         kn[i] = load4(static_cast<const float*>(a.kv.k) + at + my_d);
         vn[i] = load4(static_cast<const float*>(a.kv.v) + at + my_d);
@@ -88,7 +90,11 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
   // Of the warp's rows (it may have none): all see the keys below `clear`, none sees one from `reach` on.
   const int first = (threadIdx.x >> 5) * 2 * RM;
   const int clear = q.cached + (a.mask ? 0 : pack.row(first) + 1);
-  const int reach = first >= live ? 0 : a.mask ? keys.hi : q.cached + pack.row(min(first + 2 * RM, live) - 1) + 1;
+  const int reach = first >= live ? 0 : a.mask ? q.cached + q.n : q.cached + pack.row(min(first + 2 * RM, live) - 1) + 1;
+  int low[RM];                                         // first positions of the rows' windows
+  const int low_warp = window_lows<kWin>(a, q, 0, pack.row(min(first + 2 * RM, live) - 1)).to;
+#pragma unroll
+  for (int r = 0; r < RM; ++r) low[r] = kWin ? window_low(a, q, pack.row(ty * RM + r)) : 0;
   for (int k0 = keys.lo; k0 < keys.hi; k0 += kFN) {
     __syncthreads();                                   // the tile before has been read
 #pragma unroll
@@ -98,7 +104,8 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
     }
     __syncthreads();
     if (k0 + kFN < keys.hi) fetch(k0 + kFN);
-    if (k0 >= reach) continue;
+    const int at0 = kWin ? gap.at(k0) : k0;            // position of the tile's first key
+    if (at0 >= reach) continue;
     float sc[RM][4];
 #pragma unroll
     for (int r = 0; r < RM; ++r)
@@ -117,7 +124,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
           sc[r][c] = fmaf(qq.x, kk[c].x, fmaf(qq.y, kk[c].y, fmaf(qq.z, kk[c].z, fmaf(qq.w, kk[c].w, sc[r][c]))));
       }
     }
-    const bool edge = k0 + kFN > clear;                // some key of the tile may be hidden from some row
+    const bool edge = at0 + kFN > clear || !in_window<kWin>(a, low_warp, at0, kFN);      // some key of the tile may be hidden from some row
 #pragma unroll
     for (int r = 0; r < RM; ++r) {
       const int row = pack.row(ty * RM + r);
@@ -125,7 +132,7 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
       float mx = -INFINITY;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        see[c] = !edge || sees(a, q, row, k0 + tx + 16 * c);
+        see[c] = !edge || sees<kWin>(a, q, row, at0 + tx + 16 * c, low[r]);
         sc[r][c] = see[c] ? sc[r][c] * a.c : -INFINITY;
         mx = fmaxf(mx, sc[r][c]);
       }
@@ -185,13 +192,13 @@ __global__ void __launch_bounds__(kFThreads, 128 / D + (RM == 1)) attn_f32_kerne
       for (int c = 0; c < kDC; ++c) *reinterpret_cast<float4*>(&os[ty * RM + r][tx * 4 + 64 * c]) = o[r][c];
       if (tx == 0) sm.m[ty * RM + r] = m[r], sm.l[ty * RM + r] = l[r];
     }
-    join_cluster<float, D>(a, q, h, pack, live, &os[0][0], D + 4, sm.m, sm.l);
+    join_cluster<float, D, kWin>(a, q, h, pack, live, &os[0][0], D + 4, sm.m, sm.l);
     return;
   }
 #pragma unroll
   for (int r = 0; r < RM; ++r) {
     if (ty * RM + r >= live) continue;
-    const float f = normaliser(a, q, pack.row(ty * RM + r), l[r]);
+    const float f = normaliser<kWin>(a, q, pack.row(ty * RM + r), l[r]);
 #pragma unroll
     for (int c = 0; c < kDC; ++c)
       store4(static_cast<float*>(a.out) + vec_at<D>(pack, q, h, ty * RM + r, a.out_stride) + tx * 4 + 64 * c,
@@ -224,7 +231,7 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
-template <int D>
+template <int D, bool kWin>
 __global__ void __launch_bounds__(kSThreads, 3)
     attn_step_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using L = SLayout<D>;
@@ -250,25 +257,29 @@ __global__ void __launch_bounds__(kSThreads, 3)
   const bool my_v = lane / kDC & 1;
   tc::pdl_wait();
   tc::pdl_trigger();
-  const int s = a.ranked ? by_tokens(a.ch, blockIdx.z) : blockIdx.z;
+  const int s = a.ranked ? by_tokens<kWin>(a, blockIdx.z) : blockIdx.z;
   const int32_t* table = a.ch.table + (long long)s * a.ch.table_stride;
   // the first tiles' pages on their way with the lengths (one part only: it starts at key 0)
   const int first_col = (warp * kSTile + my_box * rows) / a.kv.page_size;
-  const int first_page = a.splits == 1 && warp < S && my_box < boxes && first_col < a.ch.table_stride ? __ldg(table + first_col) : 0;
+  const int first_page = !kWin && a.splits == 1 && warp < S && my_box < boxes && first_col < a.ch.table_stride ? __ldg(table + first_col) : 0;
   const Seq q = load_seq(a.ch, s);
   if (q.n < 0 && split == 0 && h == 0 && threadIdx.x == 0) report(a.err, MCD_ERR_INVALID_ARG);
   if (q.n <= 0 || q.n > kSVecs / a.group) return;      // (more: the chunk kernel's)
   const int vecs = q.n * a.group;
   const Pack pack(0, a.group);
-  const Span keys = part_of(q.cached + q.n, split, a.splits, kSTile);
+  const Lows lows = window_lows<kWin>(a, q, 0, q.n - 1);
+  const Gap gap = gap_of<kWin>(a, lows.from, kSTile);
+  const Span keys = part_of(q.cached + q.n - gap.gap, split, a.splits, kSTile);
   const int n_tiles = (keys.hi - keys.lo + kSTile - 1) / kSTile;
   __syncthreads();                                     // the barriers
 
   // Tile t into its stage, by one warp.
   auto load_tile = [&](int t, bool first) {
-    const int pos = keys.lo + t * kSTile + my_box * rows;
-    const bool mine = my_box < boxes && pos < keys.hi;
-    int page = !mine ? 0 : first && a.splits == 1 ? first_page : __ldg(table + pos / a.kv.page_size);
+    const int from = keys.lo + t * kSTile, pos = (kWin ? gap.at(from) : from) + my_box * rows;
+    const bool mine = my_box < boxes && from + my_box * rows < keys.hi;
+    // (a box that no row sees takes the page of one that some row does: its own may be gone)
+    const int of = touched<kWin>(a, lows.from, pos, rows) ? pos : lows.from;
+    int page = !mine ? 0 : !kWin && first && a.splits == 1 ? first_page : __ldg(table + of / a.kv.page_size);
     if (page < 0 || page >= a.kv.n_pages) {
       report(a.err, MCD_ERR_INVALID_ARG);
       page = 0;
@@ -303,6 +314,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
   // rows of the vectors (none: nobody reads what such a vector gives)
   const int i0 = r0 < vecs ? pack.row(r0) : -1, i1 = r1 < vecs ? pack.row(r1) : -1;
+  const int low0 = kWin && i0 >= 0 ? window_low(a, q, i0) : 0, low1 = kWin && i1 >= 0 ? window_low(a, q, i1) : 0;
 
   bool ok = true;
   for (int t = 0; t < n_tiles; ++t) {
@@ -310,9 +322,9 @@ __global__ void __launch_bounds__(kSThreads, 3)
     ok = ok && warp_wait(&full[t % S], t / S & 1, a.err, &abort_flag);
     uint8_t* const v_tile = smem + t % S * L::kStage + L::kHalf;
     const uint32_t vs = smem_u32(v_tile), ks = vs - L::kHalf;
-    const int key0 = keys.lo + t * kSTile + 16 * warp;
-    if (key0 + 16 > keys.hi) {                         // values behind the keys: zeros
-      for (int i = max(0, keys.hi - key0) * 8 + lane; i < 16 * 8; i += 32)
+    const int from = keys.lo + t * kSTile, key0 = (kWin ? gap.at(from) : from) + 16 * warp, left = keys.hi - from - 16 * warp;
+    if (left < 16) {                                   // values behind the keys: zeros
+      for (int i = max(0, left) * 8 + lane; i < 16 * 8; i += 32)
         for (int c = 0; c < kDC; ++c) *reinterpret_cast<uint4*>(v_tile + c * kChunk + 16 * warp * 128 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
       __syncwarp();
     }
@@ -329,7 +341,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
         mma_bf16_16816(z[1], qf[i], b[2], b[3]);
       }
     }
-    const bool edge = key0 + 16 > q.cached;
+    const bool cut = !in_window<kWin>(a, lows.to, key0, 16), edge = key0 + 16 > q.cached || cut;
     unsigned hidden = 0;                               // bit 4 n + e: z[n][e] is hidden
     if (edge) {
 #pragma unroll
@@ -337,7 +349,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = e < 2 ? i0 : i1;
-          if (i >= 0 && !sees(a, q, i, key0 + 8 * n + 2 * (lane & 3) + (e & 1))) hidden |= 1u << (4 * n + e);
+          if (i >= 0 && !sees<kWin>(a, q, i, key0 + 8 * n + 2 * (lane & 3) + (e & 1), e < 2 ? low0 : low1)) hidden |= 1u << (4 * n + e);
         }
     }
     float x0 = -INFINITY, x1 = -INFINITY;
@@ -376,10 +388,10 @@ __global__ void __launch_bounds__(kSThreads, 3)
         lo[2 * n + e / 2] = pack_bf16x2(u - bf16_lo_f32(x), w - bf16_hi_f32(x));
       }
     // A product would take an infinity or NaN of a hidden key's value into the row (0 * inf): where one of
-    // the tile's new rows has such a value, the sums skip hidden keys one by one.
+    // the tile's new rows (of its keys, where the window ends in it) has such a value, the sums skip hidden keys one by one.
     bool odd = false;
     if (edge && __any_sync(0xffffffffu, hidden)) {
-      const int first = max(q.cached - key0, 0), n = (min(keys.hi - key0, 16) - first) * 8;
+      const int first = cut ? 0 : max(q.cached - key0, 0), n = (min(left, 16) - first) * 8;
       for (int i = lane; i < n; i += 32)
         for (int c = 0; c < kDC; ++c) {
           const uint4 v = *reinterpret_cast<const uint4*>(v_tile + c * kChunk + (16 * warp + first) * 128 + i * 16);
@@ -462,7 +474,7 @@ __global__ void __launch_bounds__(kSThreads, 3)
       x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     }
     if (a.splits == 1) {
-      const float f = normaliser(a, q, pack.row(r), sum);
+      const float f = normaliser<kWin>(a, q, pack.row(r), sum);
       store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
     } else if (a.part) {
       float* to = a.part + ((pair * a.splits + split) * kSVecs + r) * (D + 4);
@@ -473,11 +485,11 @@ __global__ void __launch_bounds__(kSThreads, 3)
       if (d == 0) fin_m[r] = mx, fin_l[r] = sum;
     }
   }
-  if (a.splits > 1 && !a.part) join_cluster<uint16_t, D>(a, q, h, pack, vecs, os, L::kPitch, fin_m, fin_l);
+  if (a.splits > 1 && !a.part) join_cluster<uint16_t, D, kWin>(a, q, h, pack, vecs, os, L::kPitch, fin_m, fin_l);
 }
 
 // Joins parts in the workspace: a CTA per (KV head, sequence), a thread per four elements of o.
-template <int D>
+template <int D, bool kWin>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
   const int h = blockIdx.x, s = blockIdx.y;
   tc::pdl_wait();
@@ -504,7 +516,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnArgs a) {
       sum = fmaf(f, ml.y, sum);
       x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
     }
-    const float f = normaliser<false>(a, q, pack.row(r), sum);
+    const float f = normaliser<kWin, false>(a, q, pack.row(r), sum);
     store4(static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
 }
@@ -525,21 +537,28 @@ int splits_for(long long work, int max_tokens, int least, int most, int ctas = 2
 // order in which they are given, 59.1.
 bool rank(const mcd_chunks& ch, long long ctas) { return ch.n_seqs > 1 && ch.n_seqs <= kRanked && ctas > 2 * sm_count(); }
 
-template <int D, int RM>
+// Keys that some row of a group of `rows` rows reads, at most: with a window not all of max_tokens.
+int most_keys(const AttnArgs& a, long long rows) {
+  return a.window ? (int)std::min<long long>(a.ch.max_tokens, (long long)a.window + a.sinks + rows) : a.ch.max_tokens;
+}
+
+template <int D, int RM, bool kWin>
 cudaError_t launch_f32(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
   const int bytes = (int)sizeof(FSmem<D, RM>);
-  cudaError_t e = opt_in(attn_f32_kernel<D, RM>, bytes, done);
+  cudaError_t e = opt_in(attn_f32_kernel<D, RM, kWin>, bytes, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((long long)a.ch.max_rows * a.group + 16 * RM - 1) / (16 * RM);
-  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, a.ch.max_tokens, 64, 8, RM == 1 ? 2 : 4);
+  a.splits = splits_for(tiles * a.kv.n_kv_heads * a.ch.n_seqs, most_keys(a, std::min(a.ch.max_rows, 16 * RM)), 64, 8, RM == 1 ? 2 : 4);
   a.ranked = rank(a.ch, tiles * a.kv.n_kv_heads * a.ch.n_seqs * a.splits);
-  return launch_clusters(attn_f32_kernel<D, RM>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
+  return launch_clusters(attn_f32_kernel<D, RM, kWin>, dim3((unsigned)(tiles * a.splits), a.kv.n_kv_heads, a.ch.n_seqs), kFThreads,
                          a.splits, bytes, st, a);
 }
 template <int D>
 cudaError_t launch_f32(const AttnArgs& a, cudaStream_t st) {
-  return (long long)a.ch.max_rows * a.group <= 16 ? launch_f32<D, 1>(a, st) : launch_f32<D, 4>(a, st);
+  const bool few = (long long)a.ch.max_rows * a.group <= 16;
+  if (a.window) return few ? launch_f32<D, 1, true>(a, st) : launch_f32<D, 4, true>(a, st);
+  return few ? launch_f32<D, 1, false>(a, st) : launch_f32<D, 4, false>(a, st);
 }
 
 struct StepPlan {
@@ -548,10 +567,11 @@ struct StepPlan {
 };
 // Up to 8 parts are joined by the CTAs of a cluster; where that leaves most SMs idle and the
 // keys are many, more parts go through the workspace.
-StepPlan plan_step(const mcd_paged_kv& kv, const mcd_chunks& ch) {
-  const long long pairs = (long long)kv.n_kv_heads * ch.n_seqs;
-  const int z = splits_for(pairs, ch.max_tokens, 64, 8);
-  const int more = splits_for(pairs, ch.max_tokens, 512, 128);
+StepPlan plan_step(const AttnArgs& a) {
+  const long long pairs = (long long)a.kv.n_kv_heads * a.ch.n_seqs;
+  const int keys = most_keys(a, std::min(a.ch.max_rows, kSVecs));
+  const int z = splits_for(pairs, keys, 64, 8);
+  const int more = splits_for(pairs, keys, 512, 128);
   return more > 8 ? StepPlan{more, true} : StepPlan{z, false};
 }
 
@@ -570,43 +590,52 @@ Route route_of(const mcd_chunks& ch, int group) {
   return {!chunks || (int64_t)ch.n_rows < (int64_t)ch.n_seqs * ch.max_rows, chunks};
 }
 
-template <int D>
+template <int D, bool kWin>
 cudaError_t launch_step(AttnArgs a, void* workspace, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
   const int bytes = SLayout<D>::kBytes, rows = std::min(a.kv.page_size, kSTile);
-  cudaError_t e = opt_in(attn_step_kernel<D>, bytes, done);
+  cudaError_t e = opt_in(attn_step_kernel<D, kWin>, bytes, done);
   if (e != cudaSuccess) return e;
   CUtensorMap k_map, v_map;
   if (!page_map(&k_map, a.kv, a.kv.k, a.layer, rows) || !page_map(&v_map, a.kv, a.kv.v, a.layer, rows)) return cudaErrorInvalidValue;
-  const StepPlan p = plan_step(a.kv, a.ch);
+  const StepPlan p = plan_step(a);
   a.splits = p.splits;
   a.ranked = rank(a.ch, (long long)a.kv.n_kv_heads * a.ch.n_seqs * p.splits);
   a.part = p.in_workspace ? static_cast<float*>(workspace) : nullptr;
-  e = launch_clusters(attn_step_kernel<D>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a, k_map,
+  e = launch_clusters(attn_step_kernel<D, kWin>, dim3(a.splits, a.kv.n_kv_heads, a.ch.n_seqs), kSThreads, a.part ? 1 : a.splits, bytes, st, a, k_map,
                       v_map);
-  if (e == cudaSuccess && a.part) e = tc::launch(true, attn_join_kernel<D>, dim3(a.kv.n_kv_heads, a.ch.n_seqs), dim3(256), 0, st, a);
+  if (e == cudaSuccess && a.part) e = tc::launch(true, attn_join_kernel<D, kWin>, dim3(a.kv.n_kv_heads, a.ch.n_seqs), dim3(256), 0, st, a);
   return e;
 }
 
-}  // namespace
-}  // namespace paged
-}  // namespace mcd
+template <int D>
+cudaError_t launch_step(const AttnArgs& a, void* workspace, cudaStream_t st) {
+  return a.window ? launch_step<D, true>(a, workspace, st) : launch_step<D, false>(a, workspace, st);
+}
 
-using namespace mcd;
+// A call's arguments as the plans look at them (a window that holds every position is none).
+AttnArgs planned(const mcd_paged_kv& kv, const mcd_chunks& ch, int group, int window, int sinks) {
+  AttnArgs a = {};
+  a.kv = kv;
+  a.ch = bounded(ch);
+  a.group = group;
+  a.splits = 1;
+  if (window > 0 && window < ch.max_tokens) a.window = window, a.sinks = std::min(sinks, ch.max_tokens);
+  return a;
+}
 
-extern "C" int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads) {
-  using namespace paged;
+// (a window of 0: none)
+int64_t workspace_bytes_of(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads, int32_t window, int32_t sinks) {
   if (check_kv(kv) != MCD_OK || check_chunks(chunks, kv) != MCD_OK || no_rows(chunks) || n_q_heads <= 0) return 0;
-  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(bounded(*chunks), std::max(1, n_q_heads / kv->n_kv_heads)).steps) return 0;
-  const StepPlan p = plan_step(*kv, *chunks);
+  const AttnArgs a = planned(*kv, *chunks, std::max(1, n_q_heads / kv->n_kv_heads), window, sinks);
+  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(a.ch, a.group).steps) return 0;
+  const StepPlan p = plan_step(a);
   return p.in_workspace ? 4ll * kv->n_kv_heads * chunks->n_seqs * p.splits * kSVecs * (kv->head_dim + 4) : 0;
 }
 
-extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks,
-                                          int32_t n_q_heads, const void* q, int64_t q_stride, void* out,
-                                          int64_t out_stride, float scale, const uint32_t* mask, int32_t mask_words,
-                                          void* workspace, int64_t workspace_bytes, int32_t* err, void* stream) {
-  using namespace paged;
+mcd_status attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads, const void* q,
+                     int64_t q_stride, void* out, int64_t out_stride, float scale, int32_t window, int32_t sinks, const uint32_t* mask,
+                     int32_t mask_words, void* workspace, int64_t workspace_bytes, int32_t* err, void* stream) {
   mcd_status s = check_kv(kv);
   if (s != MCD_OK) return s;
   if ((s = check_chunks(chunks, kv)) != MCD_OK) return s;
@@ -621,10 +650,13 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
   if (q_stride < width || out_stride < width) return MCD_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || q_stride * esize(kv->dtype) % 16 || out_stride * esize(kv->dtype) % 16)
     return MCD_ERR_UNSUPPORTED;
-  const int64_t need = mcd_paged_attention_workspace(kv, chunks, n_q_heads);
+  const int64_t need = workspace_bytes_of(kv, chunks, n_q_heads, window, sinks);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
-  const AttnArgs a{*kv, bounded(*chunks), q, out, mask, err, q_stride, out_stride, layer, n_q_heads / kv->n_kv_heads, mask_words, 1, 0, nullptr,
-                   scale * 1.4426950408889634f, 0};
+  AttnArgs a = planned(*kv, *chunks, n_q_heads / kv->n_kv_heads, window, sinks);
+  a.q = q, a.out = out, a.mask = mask, a.err = err;
+  a.q_stride = q_stride, a.out_stride = out_stride;
+  a.layer = layer, a.mask_words = mask_words;
+  a.c = scale * 1.4426950408889634f;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (kv->dtype == MCD_WEIGHT_F32)
     return cuda_status(kv->head_dim == 64 ? launch_f32<64>(a, st) : launch_f32<128>(a, st));
@@ -637,4 +669,37 @@ extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer,
     e = launch_chunk(b, st);
   }
   return cuda_status(e);
+}
+
+}  // namespace
+}  // namespace paged
+}  // namespace mcd
+
+using namespace mcd;
+
+extern "C" int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads) {
+  return paged::workspace_bytes_of(kv, chunks, n_q_heads, 0, 0);
+}
+
+extern "C" mcd_status mcd_paged_attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks,
+                                          int32_t n_q_heads, const void* q, int64_t q_stride, void* out,
+                                          int64_t out_stride, float scale, const uint32_t* mask, int32_t mask_words,
+                                          void* workspace, int64_t workspace_bytes, int32_t* err, void* stream) {
+  return paged::attention(kv, layer, chunks, n_q_heads, q, q_stride, out, out_stride, scale, 0, 0, mask, mask_words, workspace,
+                          workspace_bytes, err, stream);
+}
+
+extern "C" int64_t mcd_paged_attention_window_workspace(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads,
+                                                        int32_t window, int32_t n_sinks) {
+  return window < 1 || n_sinks < 0 ? 0 : paged::workspace_bytes_of(kv, chunks, n_q_heads, window, n_sinks);
+}
+
+extern "C" mcd_status mcd_paged_attention_window(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks,
+                                                 int32_t n_q_heads, const void* q, int64_t q_stride, void* out,
+                                                 int64_t out_stride, float scale, int32_t window, int32_t n_sinks,
+                                                 const uint32_t* mask, int32_t mask_words, void* workspace,
+                                                 int64_t workspace_bytes, int32_t* err, void* stream) {
+  if (window < 1 || n_sinks < 0) return MCD_ERR_INVALID_ARG;
+  return paged::attention(kv, layer, chunks, n_q_heads, q, q_stride, out, out_stride, scale, window, n_sinks, mask, mask_words,
+                          workspace, workspace_bytes, err, stream);
 }

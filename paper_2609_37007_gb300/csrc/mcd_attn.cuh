@@ -32,14 +32,24 @@ struct AttnArgs {
   float* part;             // workspace of the parts (null: the CTAs of a cluster join them)
   float c;                 // scale * log2(e)
   int ranked;              // sequences are taken in the order of their tokens (by_tokens)
+  int window, sinks;       // kernels with a window (kWin)
 };
 
 // CTAs start in the order of their numbers, and a long one that starts last is waited for alone: the sequences with most
 // tokens come first.
 constexpr int kRanked = 128;           // sequences that are put in order
 
+// Keys that a sequence's rows read, for that order.
+template <bool kWin>
+__device__ __forceinline__ int tokens_of(const AttnArgs& a, const Seq& q) {
+  const int n = q.cached + q.n;
+  return kWin ? (int)min((long long)n, (long long)a.window + a.sinks + q.n) : n;
+}
+
 // The sequence of rank `at`, ties in the order of their numbers.  The whole block calls it, of kRanked threads at least.
-__device__ __forceinline__ int by_tokens(const mcd_chunks& ch, int at) {
+template <bool kWin>
+__device__ __forceinline__ int by_tokens(const AttnArgs& a, int at) {
+  const mcd_chunks& ch = a.ch;
   __shared__ __align__(16) int tokens[kRanked];
   __shared__ int found;
   const int i = threadIdx.x;
@@ -47,7 +57,7 @@ __device__ __forceinline__ int by_tokens(const mcd_chunks& ch, int at) {
   if (i < kRanked) {
     if (i < ch.n_seqs) {
       const Seq q = load_seq(ch, i);
-      mine = q.n > 0 ? q.cached + q.n : 0;
+      mine = q.n > 0 ? tokens_of<kWin>(a, q) : 0;
     }
     tokens[i] = mine;
   }
@@ -65,12 +75,60 @@ __device__ __forceinline__ int by_tokens(const mcd_chunks& ch, int at) {
   return __reduce_max_sync(0xffffffffu, found);        // (a uniform register)
 }
 
-// Whether packed vectors of row i (of the sequence's new rows) see key `pos`; keys below q.cached are seen by all.
-__device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int pos) {
+// With a window, a row at position p sees of the cached positions (without a mask of all) those from p - window + 1 on and the
+// first `sinks`.  p is the row's slot, with a mask the number of new rows that it sees, less one, behind the cached ones.
+// The first position of row i's window:
+__device__ __forceinline__ int window_low(const AttnArgs& a, const Seq& q, int i) {
+  int p = q.cached + i;
+  if (a.mask && i < q.n) {
+    const uint32_t* row = a.mask + (long long)(q.row0 + i) * a.mask_words;
+    int n = 0;
+    for (int j = 0; j < q.n; j += 32) n += __popc(__ldg(row + (j >> 5)) & (q.n - j >= 32 ? 0xffffffffu : (1u << (q.n - j)) - 1u));
+    p = q.cached + max(n, 1) - 1;
+  }
+  return max(0, p - a.window + 1);
+}
+// ... and bounds of it over rows i0 .. i1: none is below `from`, none above `to`.
+struct Lows {
+  int from, to;
+};
+template <bool kWin>
+__device__ __forceinline__ Lows window_lows(const AttnArgs& a, const Seq& q, int i0, int i1) {
+  if (!kWin) return {0, 0};
+  return {max(0, q.cached + (a.mask ? 0 : i0) - a.window + 1), max(0, q.cached + (a.mask ? q.n - 1 : i1) - a.window + 1)};
+}
+// Positions between the sinks and the first window are left out, in whole tiles: key v of what is read stands at position
+// v below `edge`, from there on at v + gap.
+struct Gap {
+  int edge, gap;
+  __device__ __forceinline__ int at(int v) const { return v >= edge ? v + gap : v; }
+};
+template <bool kWin>
+__device__ __forceinline__ Gap gap_of(const AttnArgs& a, int low, int tile) {
+  if (!kWin) return {0, 0};
+  const int edge = (int)(((long long)a.sinks + tile - 1) / tile * tile), start = low / tile * tile;
+  return start > edge ? Gap{edge, start - edge} : Gap{0, 0};
+}
+// Whether some row whose window starts at `low` or later sees one of the n positions from pos on.
+template <bool kWin>
+__device__ __forceinline__ bool touched(const AttnArgs& a, int low, int pos, int n) {
+  return !kWin || pos + n > low || pos < a.sinks;
+}
+// Whether a window that starts at `low` or before hides none of the n positions from pos on.
+template <bool kWin>
+__device__ __forceinline__ bool in_window(const AttnArgs& a, int low, int pos, int n) {
+  return !kWin || pos >= low || pos + n <= a.sinks;
+}
+
+// Whether packed vectors of row i (of the sequence's new rows) see key `pos`; without a window keys below q.cached are seen by
+// all (low: the row's window_low).
+template <bool kWin>
+__device__ __forceinline__ bool sees(const AttnArgs& a, const Seq& q, int i, int pos, int low = 0) {
   const int j = pos - q.cached;
-  if (j < 0) return true;
+  const bool near = in_window<kWin>(a, low, pos, 1);
+  if (j < 0) return near;
   if (j >= q.n || i >= q.n) return false;
-  if (!a.mask) return j <= i;
+  if (!a.mask) return j <= i && near;
   return (__ldg(a.mask + (long long)(q.row0 + i) * a.mask_words + (j >> 5)) >> (j & 31)) & 1u;
 }
 
@@ -83,10 +141,11 @@ __device__ __forceinline__ float without_weights(const uint32_t* mask_row, int n
 }
 // (behind a call: in line it takes the chunk and step kernels' last registers, 1 % of their time)
 static __device__ __noinline__ float without_weights_call(const uint32_t* mask_row, int n) { return without_weights(mask_row, n); }
-template <bool kCall = true>
+template <bool kWin, bool kCall = true>
 __device__ __forceinline__ float normaliser(const AttnArgs& a, const Seq& q, int i, float l) {
   if (l != 0.f) return 1.f / l;
-  if (!a.mask || q.cached > 0) return NAN;             // (without a mask it sees itself)
+  if (!a.mask) return NAN;                             // (it sees itself)
+  if (q.cached > 0 && (!kWin || a.sinks > 0 || window_low(a, q, i) < q.cached)) return NAN;
   const uint32_t* row = a.mask + (long long)(q.row0 + i) * a.mask_words;
   return kCall ? without_weights_call(row, q.n) : without_weights(row, q.n);
 }
@@ -179,7 +238,7 @@ __device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int 
 // Joins the parts of `vecs` packed vectors that the CTAs of a cluster hold in the same places of their shared
 // memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
 // m = -inf and l = 0.
-template <class T, int D>
+template <class T, int D, bool kWin>
 __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, const Pack& pack, int vecs, float* o, int pitch,
                                              float* m, float* l) {
   namespace cg = cooperative_groups;
@@ -199,7 +258,7 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, in
       sum = fmaf(w, *cl.map_shared_rank(l + r, z), sum);
       x.x = fmaf(w, y.x, x.x), x.y = fmaf(w, y.y, x.y), x.z = fmaf(w, y.z, x.z), x.w = fmaf(w, y.w, x.w);
     }
-    const float f = normaliser(a, q, pack.row(r), sum);
+    const float f = normaliser<kWin>(a, q, pack.row(r), sum);
     store4(static_cast<T*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
   cl.sync();                                           // nobody leaves while others read

@@ -122,16 +122,18 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// Bits of the positions pos0 .. pos0 + 31 that row i sees.
-__device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, int i, int pos0) {
+// Bits of the positions pos0 .. pos0 + 31 that row i sees (its window starts at `low`).
+template <bool kWin>
+__device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, int i, int pos0, int low) {
   const int j0 = pos0 - q.cached;                      // new row of bit 0
   auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
   if (i >= q.n) return 0u;
-  if (!a.mask) return below(i + 1 - j0);
-  if (j0 <= -32) return 0xffffffffu;
+  const uint32_t near = kWin ? ~below(low - pos0) | below(a.sinks - pos0) : 0xffffffffu;
+  if (!a.mask) return below(i + 1 - j0) & near;
+  if (j0 <= -32) return near;
   const uint32_t* row = a.mask + (long long)(q.row0 + i) * a.mask_words;
   const uint32_t in = below(q.n - j0);
-  if (j0 < 0) return (below(-j0) | __ldg(row) << -j0) & in;
+  if (j0 < 0) return ((below(-j0) & near) | __ldg(row) << -j0) & in;
   if (!in) return 0u;
   const int w = j0 >> 5;                               // (w < ceil(n / 32) <= mask_words)
   const uint32_t next = w + 1 < a.mask_words ? __ldg(row + w + 1) : 0u;
@@ -139,17 +141,19 @@ __device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, i
 }
 
 // Packed vector r of the pair over the keys of `keys`, key by key, by a warp; lane d holds dimensions d * D / 32 ...
-template <int D>
-__device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, const Pack& pack, int r, Span keys, float& m, float& l,
-                                      float (&o)[D / 32]) {
+template <int D, bool kWin>
+__device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, const Pack& pack, int r, Span keys, Gap gap, float& m,
+                                      float& l, float (&o)[D / 32]) {
   constexpr int kE = D / 32;
   const int lane = threadIdx.x & 31, i = pack.row(r);
   const uint16_t* qp = static_cast<const uint16_t*>(a.q) + vec_at<D>(pack, q, h, r, a.q_stride) + lane * kE;
   float x[kE];
   for (int e = 0; e < kE; ++e) x[e] = bf16_bits_to_f32(qp[e]), o[e] = 0.f;
   m = -INFINITY, l = 0.f;
-  for (int pos = keys.lo; pos < keys.hi; ++pos) {
-    if (!sees(a, q, i, pos)) continue;
+  const int low = kWin ? window_low(a, q, i) : 0;
+  for (int n = keys.lo; n < keys.hi; ++n) {
+    const int pos = kWin ? gap.at(n) : n;
+    if (!sees<kWin>(a, q, i, pos, low)) continue;
     const long long at = key_at(a, s, h, pos);
     if (at < 0) continue;
     const uint16_t* kp = static_cast<const uint16_t*>(a.kv.k) + at + lane * kE;
@@ -158,10 +162,10 @@ __device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, in
     for (int e = 0; e < kE; ++e) z = fmaf(x[e], bf16_bits_to_f32(kp[e]), z);
     for (int w = 16; w; w >>= 1) z += __shfl_xor_sync(0xffffffffu, z, w);
     z *= a.c;
-    const float n = fmaxf(m, z), base = n == -INFINITY ? 0.f : n, f = exp2f(m - base), u = exp2f(z - base);
+    const float mn = fmaxf(m, z), base = mn == -INFINITY ? 0.f : mn, f = exp2f(m - base), u = exp2f(z - base);
     l = l * f + u;
     for (int e = 0; e < kE; ++e) o[e] = o[e] * f + u * bf16_bits_to_f32(vp[e]);
-    m = n;
+    m = mn;
   }
 }
 
@@ -173,6 +177,7 @@ __device__ __forceinline__ int pairs_of(const AttnArgs& a, const Seq& q) {
 
 // Sequence of pair `slot` and the pair's number in it (an empty slot: -1, or too large).  The whole block calls it;
 // seen: shared memory of kRanked + 1 entries.
+template <bool kWin>
 __device__ __forceinline__ int2 find_pair(const AttnArgs& a, long long slot, int2* seen) {
   if (a.ranked) {
     // sequences in the order of their tokens, ties in that of their numbers.  Where do i's pairs start?  A warp asks, its
@@ -182,7 +187,7 @@ __device__ __forceinline__ int2 find_pair(const AttnArgs& a, long long slot, int
     int2 mine = make_int2(0, 0);                       // tokens and pairs
     if (i < a.ch.n_seqs) {
       const Seq q = load_seq(a.ch, i);
-      mine = make_int2(q.cached + q.n, pairs_of(a, q));
+      mine = make_int2(tokens_of<kWin>(a, q), pairs_of(a, q));
     }
     if (i < kRanked) seen[i] = mine;                   // (behind the last sequence: no pairs)
     if (i == 0) *found = make_int2(0, -1);
@@ -211,7 +216,7 @@ __device__ __forceinline__ int2 find_pair(const AttnArgs& a, long long slot, int
   return make_int2(s, (int)max(-1ll, min(slot - first_slot(s), 0x7fffffffll)));
 }
 
-template <int D>
+template <int D, bool kWin>
 __global__ void __launch_bounds__(kCThreads, 1)
     attn_chunk_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                       const __grid_constant__ CUtensorMap q_map, const int q_boxes) {
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
   // starts last is waited for alone.
   const int part = blockIdx.x % a.splits, h = blockIdx.x / a.splits % a.kv.n_kv_heads;
   const long long slot = blockIdx.x / a.splits / a.kv.n_kv_heads;
-  const int2 found = find_pair(a, slot, reinterpret_cast<int2*>(sm_m));
+  const int2 found = find_pair<kWin>(a, slot, reinterpret_cast<int2*>(sm_m));
   const int s = __reduce_max_sync(0xffffffffu, found.x), local = __reduce_max_sync(0xffffffffu, found.y);      // (uniform registers)
   const Seq q = load_seq(a.ch, s);
   if (blockIdx.x == 0)
@@ -294,21 +299,30 @@ __global__ void __launch_bounds__(kCThreads, 1)
     return a.mask ? q.cached + q.n : q.cached + pack.row(min(r, n_vecs) - 1) + 1;
   };
   const bool two = kCTile < n_vecs;                    // tile b has rows
-  const Span keys = part_of(keys_below(kCRows), part, a.splits, kCTile);
+  const Lows lows = window_lows<kWin>(a, q, i_first, pack.row(n_vecs - 1));
+  const Gap gap = gap_of<kWin>(a, lows.from, kCTile);
+  const Span keys = part_of(keys_below(kCRows) - gap.gap, part, a.splits, kCTile);
   auto tiles_of = [&](int hi) { return max(0, (min(hi, keys.hi) - keys.lo + kCTile - 1) / kCTile); };
-  const int n_tiles = tiles_of(keys.hi), n_a = tiles_of(keys_below(kCTile)), n_b = two ? n_tiles : 0;
+  const int n_tiles = tiles_of(keys.hi), n_a = tiles_of(keys_below(kCTile) - gap.gap), n_b = two ? n_tiles : 0;
   // Tiles whose V warp 10 looks at, from this one on: those that end behind the keys or hold a key that some row does
   // not see.  Number n of these has barriers n % (S / 2) of its own (no more V tiles are in the ring): warp 10 waits
   // for every phase of them, as it could not for the ring's, whose earlier phases it has no part in.
-  const int first_look = max(0, (min(keys.hi, q.cached + (a.mask ? 0 : i_first + 1)) - keys.lo) / kCTile);
+  // With a window also the first ones, up to the last window's start: `early` of them, in whole rounds of the ring (or all),
+  // so that the ring's barriers are the same number of phases, `late`, behind the rounds in every V stage.
+  const int seen_by_all = max(0, (min(keys.hi, q.cached + (a.mask ? 0 : i_first + 1) - gap.gap) - keys.lo) / kCTile);
+  int early = 0;
+  if (kWin) early = min(n_tiles, (max(0, (lows.to - gap.gap - keys.lo + kCTile - 1) / kCTile) + S / 2 - 1) / (S / 2) * (S / 2));
+  const uint32_t late = kWin ? early / (S / 2) & 1 : 0;
+  const int first_look = max(seen_by_all, early);
 
   const uint32_t tmem = *tmem_slot;
   auto s_col = [&](int w) { return tmem + 128u * w; };
   auto o_col = [&](int w) { return tmem + 256u + 128u * w; };
   // load 2 j is K of tile j, 2 j + 1 its V; the barrier that its bytes complete, and the phase
-  auto look = [&](uint32_t i) { return i & 1 ? (int)(i >> 1) - first_look : -1; };
+  auto look_tile = [&](int j) { return j >= first_look ? j - first_look + early : j < early ? j : -1; };
+  auto look = [&](uint32_t i) { return i & 1 ? look_tile((int)(i >> 1)) : -1; };
   auto load_bar = [&](uint32_t i) { return look(i) < 0 ? &full[i % S] : &v_full[look(i) % (S / 2)]; };
-  auto load_phase = [&](uint32_t i) { return look(i) < 0 ? i / S & 1 : (uint32_t)look(i) / (S / 2) & 1; };
+  auto load_phase = [&](uint32_t i) { return look(i) < 0 ? (i / S & 1) ^ (late & i) : (uint32_t)look(i) / (S / 2) & 1; };
   auto stage = [&](uint32_t i) { return smem + L::kRing + i % S * L::kTileBytes; };
 
   float m = -INFINITY, l = 0.f;                        // softmax threads: of their row
@@ -326,9 +340,11 @@ __global__ void __launch_bounds__(kCThreads, 1)
     }
     __syncwarp();
     for (int j = 0; j < n_tiles; ++j) {
-      const int pos = keys.lo + j * kCTile + box * a.kv.page_size;
-      const bool mine = box < boxes && pos < keys.hi;
-      int page = mine ? __ldg(table + pos / a.kv.page_size) : 0;
+      const int from = keys.lo + j * kCTile, pos = (kWin ? gap.at(from) : from) + box * a.kv.page_size;
+      const bool mine = box < boxes && from + box * a.kv.page_size < keys.hi;
+      // (a page that no row sees may be gone: one that some row does takes its place)
+      const int of = touched<kWin>(a, lows.from, pos, a.kv.page_size) ? pos : lows.from;
+      int page = mine ? __ldg(table + of / a.kv.page_size) : 0;
       if (page < 0 || page >= a.kv.n_pages) {
         report(a.err, MCD_ERR_INVALID_ARG);
         page = 0;
@@ -400,8 +416,8 @@ __global__ void __launch_bounds__(kCThreads, 1)
       for (int j = 0; j < n_tiles; ++j) {
         const uint32_t at_k = at_v + 1 < S ? at_v + 1 : 0;
         if (j + 1 < n_tiles && !wait(&full[at_k], at_k ? phase : phase ^ 1)) break;
-        if (const int n = j - first_look; n < 0) {
-          if (!wait(&full[at_v], phase)) break;
+        if (const int n = look_tile(j); n < 0) {
+          if (!wait(&full[at_v], phase ^ late)) break;
         } else if (!wait(&v_full[n % (S / 2)], n / (S / 2) & 1) || !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) {
           break;
         }
@@ -419,11 +435,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
     __syncwarp();
   } else if (warp == 10) {
     // ---- V tiles that are seen in part
-    for (int j = first_look; j < n_tiles; ++j) {
+    for (int j = early > 0 ? 0 : first_look; j < n_tiles; j = j + 1 == early ? first_look : j + 1) {
       const uint32_t i = 2 * j + 1;
       if (!warp_wait(load_bar(i), load_phase(i), a.err, abort_flag)) break;
       uint8_t* v = stage(i);
-      const int k0 = keys.lo + j * kCTile, first = max(0, q.cached - k0), end = min(kCTile, keys.hi - k0);
+      const int from = keys.lo + j * kCTile, k0 = kWin ? gap.at(from) : from;
+      const int first = j < early ? 0 : max(0, q.cached - k0), end = min(kCTile, keys.hi - from);
       bool bad = false;
 #pragma unroll 4
       for (int n = first * 8 + lane; n < end * 8; n += 32)
@@ -436,7 +453,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         for (int c = 0; c < kDC; ++c) *reinterpret_cast<uint4*>(v + c * kChunk + n * 16) = make_uint4(0u, 0u, 0u, 0u);
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&v_seen[(j - first_look) % (S / 2)]);
+      if (lane == 0) mbar_arrive(&v_seen[look_tile(j) % (S / 2)]);
     }
   } else {
     // ---- softmax: thread t of tile w has row t
@@ -466,6 +483,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const bool live = base < n_vecs;
     // keys below this position are seen by every row of the warp
     const int clear = q.cached + (a.mask ? 0 : pack.row(base) + 1);
+    const int low = kWin ? window_low(a, q, row) : 0, low_warp = window_lows<kWin>(a, q, 0, pack.row(min(base + 32, n_vecs) - 1)).to;
     float mc = 0.f;                                    // c * (the maximum in use)
     bool ok = true;
     for (int j = 0; j < n_mine; ++j) {
@@ -483,12 +501,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
         for (int c = 0; c < 4; ++c) tmem_ld32(s_col(w) + lanes + 32 * c, x[c]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_loaded(x[c]);
-        const int k0 = keys.lo + j * kCTile;
-        if (k0 + kCTile > min(clear, keys.hi)) {
+        const int from = keys.lo + j * kCTile, k0 = kWin ? gap.at(from) : from;
+        if (k0 + kCTile > clear || from + kCTile > keys.hi || !in_window<kWin>(a, low_warp, k0, kCTile)) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const int pos = k0 + 32 * c, left = keys.hi - pos;
-            uint32_t see = seen_word(a, q, row, pos);
+            const int pos = k0 + 32 * c, left = keys.hi - from - 32 * c;
+            uint32_t see = seen_word<kWin>(a, q, row, pos, low);
             see &= left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[c][e] = see >> e & 1u ? x[c][e] : 0xff800000u;
@@ -580,15 +598,15 @@ __global__ void __launch_bounds__(kCThreads, 1)
         for (int r = 0; r < 32; ++r) {
           if (base + r >= n_vecs) break;
           float sl, sm, o[D / 32];
-          slow_row<D>(a, q, s, h, pack, base + r, keys, sm, sl, o);
-          const float f = normaliser(a, q, pack.row(base + r), sl);
+          slow_row<D, kWin>(a, q, s, h, pack, base + r, keys, gap, sm, sl, o);
+          const float f = normaliser<kWin>(a, q, pack.row(base + r), sl);
           uint16_t* to = static_cast<uint16_t*>(a.out) + vec_at<D>(pack, q, h, base + r, a.out_stride) + lane * (D / 32);
           for (int e = 0; e < D / 32; ++e) to[e] = (uint16_t)pack_bf16x2(o[e] * f, 0.f);
         }
       } else {
         // through the place of the tile's Q (its products are done), so that the lanes write rows and not columns: 1.4 us
         // a CTA otherwise
-        const float f = normaliser(a, q, row, l);
+        const float f = normaliser<kWin>(a, q, row, l);
         constexpr int kC = D / 8;                      // 16-byte pieces of a row
         uint4* rows = reinterpret_cast<uint4*>(smem + w * L::kTileBytes) + (warp & 3) * 32 * kC;
 #pragma unroll 1
@@ -630,7 +648,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
       if (some && *odd) {
         for (int n = 0; n < 32 && base + n < n_vecs; ++n) {
           float sm, sl, o[D / 32];
-          slow_row<D>(a, q, s, h, pack, base + n, keys, sm, sl, o);
+          slow_row<D, kWin>(a, q, s, h, pack, base + n, keys, gap, sm, sl, o);
           for (int e = 0; e < D / 32; ++e) os[(base + n) * L::kPitch + lane * (D / 32) + e] = o[e];
           if (lane == 0) sm_m[base + n] = sm, sm_l[base + n] = sl;
         }
@@ -651,7 +669,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         sm_l[r] = some ? l : 0.f;
       }
     }
-    join_cluster<uint16_t, D>(a, q, h, pack, n_vecs, os, L::kPitch, sm_m, sm_l);
+    join_cluster<uint16_t, D, kWin>(a, q, h, pack, n_vecs, os, L::kPitch, sm_m, sm_l);
     tc::tc_fence_before();
     __syncthreads();
   }
@@ -672,10 +690,10 @@ bool rows_map(CUtensorMap* map, const AttnArgs& a) {
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, bool kWin>
 cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
-  cudaError_t e = opt_in(attn_chunk_kernel<D>, CLayout<D>::kBytes, done);
+  cudaError_t e = opt_in(attn_chunk_kernel<D, kWin>, CLayout<D>::kBytes, done);
   if (e != cudaSuccess) return e;
   CUtensorMap k_map, v_map;
   if (!page_map(&k_map, a.kv, a.kv.k, a.layer, a.kv.page_size) ||
@@ -686,9 +704,10 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   if (q_boxes && !rows_map(&q_map, a)) return cudaErrorInvalidValue;
   const long long slots = (long long)a.ch.n_rows * a.group / kCRows + a.ch.n_seqs;
   const long long pairs = std::min(slots, a.ch.n_seqs * (((long long)a.ch.max_rows * a.group + kCRows - 1) / kCRows));
+  const long long keys = kWin ? std::min<long long>(a.ch.max_tokens, (long long)a.window + a.sinks + kCRows / a.group) : a.ch.max_tokens;
   // one CTA an SM: parts as long as they leave no SM two, each of two tiles at least
   a.splits = 1;
-  while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && a.ch.max_tokens / (2 * a.splits) >= 2 * kCTile)
+  while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && keys / (2 * a.splits) >= 2 * kCTile)
     a.splits *= 2;
   // Order costs a CTA 25 ns a sequence, and what it saves is the last CTAs' time: worth it for few of either (65 rows over 200
   // to 1,500 keys each: 32 sequences 45.4 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
@@ -696,7 +715,7 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   // (ordered sequences leave no slots between them)
   const long long grid = (a.ranked ? pairs : slots) * a.kv.n_kv_heads * a.splits;
   if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  return launch_clusters(attn_chunk_kernel<D>, dim3((unsigned)grid), kCThreads, a.splits, CLayout<D>::kBytes, st, a, k_map, v_map, q_map, q_boxes);
+  return launch_clusters(attn_chunk_kernel<D, kWin>, dim3((unsigned)grid), kCThreads, a.splits, CLayout<D>::kBytes, st, a, k_map, v_map, q_map, q_boxes);
 }
 
 }  // namespace
@@ -726,7 +745,8 @@ bool page_map(CUtensorMap* map, const mcd_paged_kv& kv, const void* pool, int la
 }
 
 cudaError_t launch_chunk(const AttnArgs& a, cudaStream_t st) {
-  return a.kv.head_dim == 64 ? launch_chunk_d<64>(a, st) : launch_chunk_d<128>(a, st);
+  if (a.window) return a.kv.head_dim == 64 ? launch_chunk_d<64, true>(a, st) : launch_chunk_d<128, true>(a, st);
+  return a.kv.head_dim == 64 ? launch_chunk_d<64, false>(a, st) : launch_chunk_d<128, false>(a, st);
 }
 
 }  // namespace paged

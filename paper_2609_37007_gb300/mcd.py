@@ -150,6 +150,8 @@ def load_library() -> ctypes.CDLL:
         "mcd_rope_append": (I32, [P, I32, P, I32, P, I64, I32, P, I64, P, P, P, P, ctypes.c_float, P, P]),
         "mcd_paged_attention": (I32, [P, I32, P, I32, P, I64, P, I64, ctypes.c_float, P, I32, P, I64, P, P]),
         "mcd_paged_attention_workspace": (I64, [P, P, I32]),
+        "mcd_paged_attention_window": (I32, [P, I32, P, I32, P, I64, P, I64, ctypes.c_float, I32, I32, P, I32, P, I64, P, P]),
+        "mcd_paged_attention_window_workspace": (I64, [P, P, I32, I32, I32]),
         "mcd_pages_fork": (I32, [P, P, P, I32, P, I32, P, I32, P, P, P, I32, P, I32, P, I64, P, P]),
         "mcd_pages_fork_workspace": (I64, [I32, I32, I32]),
         "mcd_pages_compact": (I32, [P, I32, P, P, I32, P, P, I32, P, P, P, P]),
@@ -481,6 +483,31 @@ def mcd_paged_attention(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: in
         None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_paged_attention", st)
+
+
+def mcd_paged_attention_window_workspace(kv: McdPagedKV, ch: McdChunks, n_q_heads: int, window: int, n_sinks: int = 0) -> int:
+    return int(load_library().mcd_paged_attention_window_workspace(kv.addr, ch.addr, n_q_heads, window, n_sinks))
+
+
+def mcd_paged_attention_window(kv: McdPagedKV, layer: int, ch: McdChunks, n_q_heads: int, q, out, scale: float, window: int, n_sinks: int,
+                               workspace, err, mask=None, stream=None):
+    """mcd_paged_attention of rows that see their last `window` positions and the first n_sinks; workspace: uint8,
+    mcd_paged_attention_window_workspace bytes, or None where that is 0.  Asynchronous."""
+    w, n = n_q_heads * kv.head_dim, ch.n_rows
+    if q.dtype is not kv.type or out.dtype is not kv.type:
+        raise ValueError("q and out have the cache's type")
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2 or mask.shape[0] < n:
+            raise ValueError("mask: [rows, words]")
+        words = mask.shape[1]
+    space, size = _space(workspace)
+    st = (_lib or load_library()).mcd_paged_attention_window(
+        kv.addr, layer, ch.addr, n_q_heads, q.data_ptr(), _rows(q, "q", n, w), out.data_ptr(), _rows(out, "out", n, w), scale, window, n_sinks,
+        None if mask is None else _i32(mask, "mask"), words, space, size, _i32(err, "err"),
+        None if stream is None else stream.cuda_stream)
+    if st:
+        _check("mcd_paged_attention_window", st)
 
 
 def mcd_pages_fork_workspace(n_src: int, table_out) -> int:

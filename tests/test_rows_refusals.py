@@ -5,7 +5,7 @@ import math
 import numpy as np
 import pytest
 
-from oracle import rows, sampler
+from oracle import paged, rows, sampler
 
 OK, INVALID, UNSUPPORTED = 0, 1, 7
 P = 1 << 20            # a 16-byte aligned address
@@ -97,3 +97,32 @@ def test_sampling_law():
     assert rows.sample(x, 0.0, 0.7, top_k=1)[0] == 1 and rows.sample(x, 0.9, 0.0)[0] == 1
     assert rows.sample(x, 0.9, 0.7, top_p=p[1] * 0.99)[3] == 1 and rows.sample(x, 0.9, 0.7, top_p=p[1] * 1.01)[3] == 2
     assert rows.sample(x, 0.9, 0.7, min_p=1.0)[3] == 2 and rows.sample(x, 0.9, 0.7)[3] == 5
+
+
+# ---- windowed attention --------------------------------------------------------------------------------
+def window_call(m, window=10, sinks=2, **k):
+    import ctypes
+    from test_cache_refusals import ch, kv
+    d, c = kv(m, **{x: k[x] for x in k if x in ("dtype", "k")}), ch(m)
+    return m.load_library().mcd_paged_attention_window(ctypes.addressof(d), 0, ctypes.addressof(c), k.get("n_q", 16), P, 2048, k.get("out", 2 * P), 2048, 0.1,
+                                                       window, sinks, k.get("mask"), k.get("words", 0), P, 1 << 40, k.get("err", P), None)
+
+
+@pytest.mark.parametrize("bad,want", [
+    (dict(window=0), INVALID), (dict(window=-5), INVALID), (dict(sinks=-1), INVALID), (dict(n_q=15), INVALID), (dict(err=None), INVALID),
+    (dict(mask=P, words=0), INVALID), (dict(out=P), INVALID), (dict(k=None), INVALID), (dict(dtype=2), UNSUPPORTED), (dict(n_q=136), UNSUPPORTED)])
+def test_window_refuses(lib, bad, want):
+    from paper_2609_37007_gb300 import mcd
+    assert window_call(mcd, **bad) == want
+
+
+def test_what_a_window_sees():
+    see = paged.seen_in_window(3, 6, 4, 1)
+    assert see.tolist() == [[True, False, False, True, True, True, True, False, False], [True, False, False, False, True, True, True, True, False],
+                            [True, False, False, False, False, True, True, True, True]]
+    assert (paged.seen_in_window(3, 6, 100, 0) == np.tril(np.ones((3, 9), bool), 6)).all()
+    tree = np.array([[1, 0, 0], [1, 1, 0], [1, 0, 1]])
+    see = paged.seen_in_window(3, 6, 4, 0, tree)
+    assert see[1, :6].tolist() == see[2, :6].tolist() == [False, False, False, False, True, True] and (see[:, 6:] == tree).all()
+    nothing = paged.seen_in_window(1, 6, 2, 0, np.array([[0]]))
+    assert nothing.tolist() == [[False] * 5 + [True, False]]
