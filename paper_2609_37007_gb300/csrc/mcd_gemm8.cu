@@ -25,7 +25,7 @@ struct Args8 {
   void* y;
   long long ldy;
   int M, N, K;
-  int pitch, splits;                   // rows of B a tile, parts of K
+  int pitch, splits, deep;             // rows of B a tile, parts of K, Layout8's kDeep
   int* err;
 };
 
@@ -112,10 +112,11 @@ __device__ __forceinline__ void store4_scaled(const Args8& g, int n, int m, floa
   }
 }
 
-template <int BN>
+// kDeep: a ring that fills an SM; without, two CTAs share one (up to 128 columns).
+template <int BN, bool kDeep>
 struct Layout8 {
   static constexpr int kABytes = kBM * kK8, kStageBytes = kABytes + BN * kK8;
-  static constexpr int kStages = BN <= 64 ? 4 : BN <= 128 ? 3 : 4;      // (two CTAs an SM up to 128 columns)
+  static constexpr int kStages = kDeep ? (kStageBudget / kStageBytes > 8 ? 8 : kStageBudget / kStageBytes) : BN <= 64 ? 4 : 3;
   static constexpr int kBar = kStages * kStageBytes;                   // full[s], empty[s], accum
   static constexpr int kMisc = kBar + (2 * kStages + 1) * 8;            // tensor memory address, abort
   static constexpr int kBytes = kMisc + 8 + 1024;                       // + alignment
@@ -127,11 +128,11 @@ struct Layout8 {
 // A tile of 128 x pitch per CTA over a part of K; the parts' CTAs are a cluster and add up through shared memory, in the
 // order of the parts.  Warp 0 copies, warp 1 multiplies, warps 2 to 5 store.
 constexpr int kThreads8 = 192, kMaxParts = 8;
-template <class T, int BN>
+template <class T, int BN, bool kDeep>
 __global__ void __launch_bounds__(kThreads8, 1)
     gemm8_tile_kernel(const Args8 g, const __grid_constant__ CUtensorMap a_map, const __grid_constant__ CUtensorMap b_map,
                       const __grid_constant__ CUtensorMap y_map) {
-  using L = Layout8<BN>;
+  using L = Layout8<BN, kDeep>;
   constexpr int S = L::kStages;
   extern __shared__ uint8_t g8_smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(g8_smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -434,13 +435,21 @@ bool map_y(CUtensorMap* map, const Args8& g) {
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class T, int BN>
+template <class T, int BN, bool kDeep>
 cudaError_t launch_tile8(const Args8& g, const CUtensorMap& a_map, const CUtensorMap& b_map, const CUtensorMap& y_map, cudaStream_t st) {
   static std::atomic<unsigned> done{0};
-  cudaError_t e = paged::opt_in(gemm8_tile_kernel<T, BN>, Layout8<BN>::kBytes, done);
+  using L = Layout8<BN, kDeep>;
+  cudaError_t e = paged::opt_in(gemm8_tile_kernel<T, BN, kDeep>, L::kBytes, done);
   if (e != cudaSuccess) return e;
-  return paged::launch_clusters(gemm8_tile_kernel<T, BN>, dim3((g.M + kBM - 1) / kBM * g.splits, (g.N + g.pitch - 1) / g.pitch), kThreads8, g.splits,
-                                Layout8<BN>::kBytes, st, g, a_map, b_map, y_map);
+  return paged::launch_clusters(gemm8_tile_kernel<T, BN, kDeep>, dim3((g.M + kBM - 1) / kBM * g.splits, (g.N + g.pitch - 1) / g.pitch), kThreads8,
+                                g.splits, L::kBytes, st, g, a_map, b_map, y_map);
+}
+template <class T>
+cudaError_t launch_tile8(const Args8& g, bool deep, const CUtensorMap& a_map, const CUtensorMap& b_map, const CUtensorMap& y_map, cudaStream_t st) {
+  if (g.pitch <= 32) return deep ? launch_tile8<T, 32, true>(g, a_map, b_map, y_map, st) : launch_tile8<T, 32, false>(g, a_map, b_map, y_map, st);
+  if (g.pitch <= 64) return deep ? launch_tile8<T, 64, true>(g, a_map, b_map, y_map, st) : launch_tile8<T, 64, false>(g, a_map, b_map, y_map, st);
+  if (g.pitch <= 128) return deep ? launch_tile8<T, 128, true>(g, a_map, b_map, y_map, st) : launch_tile8<T, 128, false>(g, a_map, b_map, y_map, st);
+  return launch_tile8<T, 256, true>(g, a_map, b_map, y_map, st);
 }
 
 // Pairs that run at a time, looked up once per device.
@@ -468,6 +477,31 @@ cudaError_t launch_pair8(const Args8& g, const CUtensorMap& a_map, const CUtenso
   return launch(true, gemm8_pair_kernel<T>, dim3(2 * pairs), dim3(kThreads8), PairLayout8::kBytes, st, g, a_map, b_map, y_map);
 }
 
+// Rows of B a tile and parts of K, by what they were measured to cost (us; 6144, 4096, 2048 and 1024 rows of A, K of 1024 to
+// 4096, 1 to 2048 rows of B): a CTA starts and ends in about 3, a slice of 128 of K takes 0.25 where a CTA has an SM to itself
+// and 0.35 where two share one, a little more with wide tiles, its columns 0.012 each to store; parts are joined in
+// 0.2 + 0.035 a column.  6144 x 4 x 1024: one part 4.7, four 3.9; 6144 x 128 x 1024: one 5.6, two 7.1.  More than four
+// thirds of the SMs' clusters do not run at a time, nor do clusters of eight that want an SM a CTA on more than half of them (2048 x 4
+// x 1024: 6.7, with two CTAs an SM 3.4).
+void plan8(Args8& g, int m_tiles, int nk, int n_sm) {
+  float best = 0.f;
+  const int rows = (g.N + 15) / 16 * 16;
+  for (int pitch : {16, 32, 64, 96, 128, 176, 256}) {
+    if (pitch > rows && pitch > 16) pitch = rows;
+    const long long tiles = (long long)m_tiles * ((g.N + pitch - 1) / pitch);
+    for (int s = 1; s <= std::min(kMaxParts, nk); s *= 2) {
+      const int per = (nk + s - 1) / s;
+      const long long ctas = tiles * s;
+      if ((nk + per - 1) / per != s || (s > 1 && 3 * ctas > 4 * n_sm)) continue;
+      const bool deep = pitch > 128 || ctas <= (s == 8 ? n_sm / 2 : n_sm);
+      const float waves = (float)((ctas + (deep ? 1 : 2) * n_sm - 1) / ((deep ? 1 : 2) * n_sm));
+      const float cost = waves * (3.f + per * (deep ? 0.25f : 0.35f) * (1.f + pitch / 512.f) + pitch * 0.012f) + (s > 1 ? 0.2f + 0.035f * pitch : 0.f);
+      if (best == 0.f || cost < best) best = cost, g.pitch = pitch, g.splits = s, g.deep = deep;
+    }
+    if (pitch == rows) break;
+  }
+}
+
 template <class T>
 cudaError_t launch8(Args8 g, const void* A, long long lda, const void* B, long long ldb, cudaStream_t st) {
   const int m_tiles = (g.M + kBM - 1) / kBM, nk = (g.K + kK8 - 1) / kK8, n_sm = paged::sm_count();
@@ -478,16 +512,9 @@ cudaError_t launch8(Args8 g, const void* A, long long lda, const void* B, long l
     if (!map8(&a_map, A, g.M, g.K, lda, kBM) || !map8(&b_map, B, g.N, g.K, ldb, kBM)) return cudaErrorInvalidValue;
     return launch_pair8<T>(g, a_map, b_map, y_map, st);
   }
-  const int n_tiles = (g.N + 255) / 256;
-  g.pitch = ((g.N + n_tiles - 1) / n_tiles + 15) / 16 * 16;
-  g.splits = std::max(1, std::min({kMaxParts, nk, n_sm / (m_tiles * n_tiles)}));
-  const int per = (nk + g.splits - 1) / g.splits;
-  g.splits = (nk + per - 1) / per;                     // (no part is empty)
+  plan8(g, m_tiles, nk, n_sm);
   if (!map8(&a_map, A, g.M, g.K, lda, kBM) || !map8(&b_map, B, g.N, g.K, ldb, g.pitch)) return cudaErrorInvalidValue;
-  if (g.pitch <= 32) return launch_tile8<T, 32>(g, a_map, b_map, y_map, st);
-  if (g.pitch <= 64) return launch_tile8<T, 64>(g, a_map, b_map, y_map, st);
-  if (g.pitch <= 128) return launch_tile8<T, 128>(g, a_map, b_map, y_map, st);
-  return launch_tile8<T, 256>(g, a_map, b_map, y_map, st);
+  return launch_tile8<T>(g, g.deep, a_map, b_map, y_map, st);
 }
 
 }  // namespace
@@ -510,7 +537,7 @@ extern "C" mcd_status mcd_tc_gemm_e4m3(int32_t M, int32_t N, int32_t K, const vo
   const rows::Block sa{a_scale, M, 1, M, 4}, sb{b_scale, N, 1, N, 4};
   for (const rows::Block* x : {&a, &b, &sa, &sb})
     if (rows::overlap(y, *x)) return MCD_ERR_INVALID_ARG;
-  const tc::Args8 g{a_scale, b_scale, Y, ldy, M, N, K, 0, 1, err};
+  const tc::Args8 g{a_scale, b_scale, Y, ldy, M, N, K, 0, 1, 0, err};
   // (a single row's stride is not looked at: the map wants one all the same)
   const int64_t la = M > 1 ? lda : (K + 15) / 16 * 16, lb = N > 1 ? ldb : (K + 15) / 16 * 16;
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -6,6 +6,7 @@
 // What bounds it: one read of x and the residual, one write of the sum and of y; for a few rows the chain load -> join -> store.
 #include <cmath>
 
+#include "mcd_cache.cuh"
 #include "mcd_rows.cuh"
 
 namespace mcd {
@@ -23,26 +24,38 @@ struct NormArgs {
   float eps, inv_width;
 };
 
-// Elements 8 c .. 8 c + 7 of a row, those from `width` on zeros.
+using paged::add2;
+using paged::fma2;
+using paged::mul2;
+using paged::pack2;
+using paged::unpack2;
+
+// Elements 8 c .. 8 c + 7 of a row in pairs, those from `width` on zeros.
 template <class T>
-__device__ __forceinline__ void load8(const void* base, long long row, long long stride, int c, int width, float (&v)[8]) {
+__device__ __forceinline__ void load8(const void* base, long long row, long long stride, int c, int width, uint64_t (&v)[4]) {
   const T* p = static_cast<const T*>(base) + row * stride + 8 * c;
+  float x[8];
   if (8 * c + 8 <= width) {
-    Vec8<T>::load(p, v);
+    Vec8<T>::load(p, x);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 8 * c + e < width ? Vec8<T>::one(p[e]) : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = 8 * c + e < width ? Vec8<T>::one(p[e]) : 0.f;
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = pack2(x[2 * e], x[2 * e + 1]);
 }
 template <class T>
-__device__ __forceinline__ void store8(void* base, long long row, long long stride, int c, int width, const float (&v)[8]) {
+__device__ __forceinline__ void store8(void* base, long long row, long long stride, int c, int width, const uint64_t (&v)[4]) {
   T* p = static_cast<T*>(base) + row * stride + 8 * c;
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) unpack2(v[e], x[2 * e], x[2 * e + 1]);
   if (8 * c + 8 <= width) {
-    Vec8<T>::store(p, v);
+    Vec8<T>::store(p, x);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (8 * c + e < width) p[e] = Vec8<T>::round(v[e]);
+      if (8 * c + e < width) p[e] = Vec8<T>::round(x[e]);
   }
 }
 
@@ -53,13 +66,12 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const N
   constexpr int kTeams = kTeam < 128 ? 128 / kTeam : 1;
   constexpr bool k8 = sizeof(TY) == 1;
   static_assert(kTeam == 32 || kTeam >= 128, "a team is a warp or a CTA");
-  const int t = threadIdx.x % kTeam;
+  const int t = threadIdx.x % kTeam, n_chunks = (a.width + 7) / 8;
   const long long row = (long long)blockIdx.x * kTeams + threadIdx.x / kTeam;
   tc::pdl_wait();
   tc::pdl_trigger();
   if (row >= a.n_rows) return;                         // (a whole team)
-  float v[kChunks][8];
-  const int n_chunks = (a.width + 7) / 8;
+  uint64_t v[kChunks][4];
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     const int c = t + i * kTeam;
@@ -67,7 +79,7 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const N
       load8<TX>(a.x, row, a.x_stride, c, a.width, v[i]);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+      for (int e = 0; e < 4; ++e) v[i][e] = 0ull;      // (two zeros)
     }
   }
   if (a.res) {
@@ -75,10 +87,10 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const N
     for (int i = 0; i < kChunks; ++i) {
       const int c = t + i * kTeam;
       if (c >= n_chunks) continue;
-      float r[8];
+      uint64_t r[4];
       load8<TR>(a.res, row, a.res_stride, c, a.width, r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] += r[e];
+      for (int e = 0; e < 4; ++e) v[i][e] = add2(v[i][e], r[e]);
     }
   }
   if (a.sum) {
@@ -88,44 +100,58 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const N
       if (c < n_chunks) store8<TR>(a.sum, row, a.sum_stride, c, a.width, v[i]);
     }
   }
-  float q = 0.f, top = 0.f;
+  uint64_t q2 = 0ull;
 #pragma unroll
   for (int i = 0; i < kChunks; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q = fmaf(v[i][e], v[i][e], q);
+    for (int e = 0; e < 4; ++e) q2 = fma2(v[i][e], v[i][e], q2);
   if (a.gain) {
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       const int c = t + i * kTeam;
       if (c >= n_chunks) continue;
-      float g[8];
+      uint64_t g[4];
       load8<float>(a.gain, 0, 0, c, a.width, g);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] *= g[e];
+      for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], g[e]);
     }
   }
-  if (k8) {
+  float q, top = 0.f;
+  {
+    float x, y;
+    unpack2(q2, x, y);
+    q = x + y;
+    if (k8) {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
+      for (int i = 0; i < kChunks; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max_nan(top, fabsf(v[i][e]));
+        for (int e = 0; e < 4; ++e) {
+          unpack2(v[i][e], x, y);
+          top = max3_nan(top, fabsf(x), fabsf(y));
+        }
+    }
   }
   // (the order of the sum is fixed by the sizes)
   team_join<kTeam, k8>(q, top);
   // (a sum that is not finite: neither is the row, where 1 / inf would leave zeros)
-  const float inv = !a.norm ? 1.f : q <= 3.40282347e38f ? 1.f / sqrtf(fmaf(q, a.inv_width, a.eps)) : NAN;
-  float back = 1.f;
+  const float inv = !a.norm ? 1.f : q <= 3.40282347e38f ? rsqrtf(fmaf(q, a.inv_width, a.eps)) : NAN;
+  float f = inv, again = 1.f;
   if (k8) {
-    const float s = max_nan(top * inv * (1.f / 448.f), 1.17549435e-38f);
+    const float s = max_nan(top * inv * (1.f / 448.f), 1.17549435e-38f), back = __fdividef(1.f, s);      // (s < 2^120: a maximum over 448)
     if (t == 0) a.scale[row] = s;
-    back = 1.f / s;
+    f = inv * back;
+    if (!(f <= 3.40282347e38f)) f = inv, again = back;      // (rows of tiny values: one after the other)
   }
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     const int c = t + i * kTeam;
     if (c >= n_chunks) continue;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * inv * back;
+    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], pack2(f, f));
+    if (k8 && again != 1.f) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], pack2(again, again));
+    }
     store8<TY>(a.y, row, a.y_stride, c, a.width, v[i]);
   }
 }
@@ -140,9 +166,10 @@ template <class TX, class TR, class TY>
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) {
   const int chunks = (a.width + 7) / 8;
   if (chunks <= 32) return launch_norm<TX, TR, TY, 32, 1>(a, st);
+  if (chunks <= 64) return launch_norm<TX, TR, TY, 32, 2>(a, st);
   if (chunks <= 128) return launch_norm<TX, TR, TY, 128, 1>(a, st);
-  if (chunks <= 256) return launch_norm<TX, TR, TY, 128, 2>(a, st);
-  if (chunks <= 512) return launch_norm<TX, TR, TY, 256, 2>(a, st);
+  if (chunks <= 256) return launch_norm<TX, TR, TY, 256, 1>(a, st);
+  if (chunks <= 512) return launch_norm<TX, TR, TY, 512, 1>(a, st);
   if (chunks <= 1024) return launch_norm<TX, TR, TY, 512, 2>(a, st);
   return launch_norm<TX, TR, TY, 1024, 2>(a, st);
 }

@@ -15,6 +15,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return d;
 }
 
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // Eight values of a type: fp32, bf16 (uint16_t) or e4m3 (uint8_t, stores only).  Rounding is to the nearest, ties to even;
 // e4m3 keeps values beyond 448 at 448.
 template <class T>
@@ -60,26 +66,23 @@ struct Vec8<uint8_t> {
   }
 };
 
-// Sum of q and (with kMax) maximum of m over a team: a warp, or the whole CTA.  Every thread of the team calls it, once.
+// Sum of q and (with kMax) maximum of m >= 0 over a team: a warp, or the whole CTA.  Every thread of the team calls it, once.
+// (Bit patterns of numbers that are not negative are in the numbers' order, NaN above all.)
 template <int kTeam, bool kMax>
 __device__ __forceinline__ void team_join(float& q, float& m) {
 #pragma unroll
-  for (int w = 16; w; w >>= 1) {
-    q += __shfl_xor_sync(0xffffffffu, q, w);
-    if (kMax) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, w));
-  }
+  for (int w = 16; w; w >>= 1) q += __shfl_xor_sync(0xffffffffu, q, w);
+  if (kMax) m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
   if (kTeam > 32) {
     constexpr int kWarps = kTeam / 32;
     __shared__ float2 part[kWarps];
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(q, m);
     __syncthreads();
-    q = 0.f;
+    const float2 p = part[threadIdx.x % kWarps];       // (every warp joins them all, each in the lanes of its kind)
+    q = p.x;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) {
-      const float2 p = part[i];
-      q += p.x;
-      if (kMax) m = max_nan(m, p.y);
-    }
+    for (int w = kWarps / 2; w; w >>= 1) q += __shfl_xor_sync(0xffffffffu, q, w);
+    if (kMax) m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(p.y)));
   }
 }
 

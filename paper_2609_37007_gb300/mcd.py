@@ -545,46 +545,51 @@ def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, 
 
 
 # ---- rows between the products (include/mcd_rows.h) and 8-bit products (include/mcd_tc.h) ----
-def _row_dtype(t) -> int:
-    if t.dtype is _E4M3:
-        return 3                    # MCD_E4M3
-    return _kv_dtype(t)
+# The same holds of these: a row's call is shorter than its checks would be with a helper for each.
+def _stride(t, n: int, w: int, what: str) -> int:
+    """Row stride (elements) of a device matrix [n, w] whose rows are contiguous."""
+    if t.shape != (n, w) or not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor [{n}, {w}]")
+    s, one = t.stride()
+    if one != 1 and w != 1:
+        raise ValueError(f"{what}: a row's elements are contiguous")
+    return s if n > 1 else max(s, w)
 
 
-def _per_row(t, dtype, what: str, n: int) -> Optional[int]:
-    """Address of n contiguous device values of a type (None: none)."""
-    if t is None:
-        return None
+def _values(t, dtype, what: str, n: int) -> int:
+    """Address of n contiguous device values of a type."""
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{what}: {n} contiguous {dtype} values on the device")
     return t.data_ptr()
 
 
-def _matrix(t, what: str) -> Tuple[int, int]:
-    if t.dim() != 2:
-        raise ValueError(f"{what}: [rows, elements]")
-    return t.shape
+def _row_dtype(t) -> int:
+    d = t.dtype
+    return 1 if d is _BF16 else 0 if d is _F32 else 3 if d is _E4M3 else _kv_dtype(t)      # MCD_WEIGHT_BF16, _F32, MCD_E4M3
 
 
 def mcd_norm_rows(x, y, residual=None, sum_out=None, gain=None, eps: float = 1e-6, norm: bool = True, y_scale=None, stream=None):
     """y [rows, width] = RMSNorm of x + residual times gain (norm False: without the norm), float32, bfloat16 or float8_e4m3fn
     with a float32 scale per row in y_scale; the sum goes to sum_out.  x, residual and sum_out float32 or bfloat16.  Asynchronous."""
-    _types()
-    n, w = _matrix(x, "x")
-    if _matrix(y, "y") != (n, w):
-        raise ValueError("y has x's shape")
-    kept = residual if sum_out is None else sum_out
-    if residual is not None and sum_out is not None and residual.dtype is not sum_out.dtype:
-        raise ValueError("residual and sum_out have one type")
-    y_dtype = _row_dtype(y)
-    if y_dtype == 3 and y_scale is None:
+    if _F32 is None:
+        _types()
+    n, w = x.shape
+    res = total = scale = None
+    rs = ss = kind = 0
+    if residual is not None:
+        res, rs, kind = residual.data_ptr(), _stride(residual, n, w, "residual"), _kv_dtype(residual)
+    if sum_out is not None:
+        total, ss, k = sum_out.data_ptr(), _stride(sum_out, n, w, "sum_out"), _kv_dtype(sum_out)
+        if res is not None and k != kind:
+            raise ValueError("residual and sum_out have one type")
+        kind = k
+    if y_scale is not None:
+        scale = _values(y_scale, _F32, "y_scale", n)
+    elif y.dtype is _E4M3:
         raise ValueError("8-bit rows need y_scale")
     st = (_lib or load_library()).mcd_norm_rows(
-        n, w, x.data_ptr(), _rows(x, "x", n, w), _kv_dtype(x), None if residual is None else residual.data_ptr(),
-        0 if residual is None else _rows(residual, "residual", n, w), None if sum_out is None else sum_out.data_ptr(),
-        0 if sum_out is None else _rows(sum_out, "sum_out", n, w), 0 if kept is None else _kv_dtype(kept), int(norm),
-        None if gain is None else _gain(gain, w), eps, y.data_ptr(), _rows(y, "y", n, w), y_dtype, _per_row(y_scale, _F32, "y_scale", n),
-        None if stream is None else stream.cuda_stream)
+        n, w, x.data_ptr(), _stride(x, n, w, "x"), _kv_dtype(x), res, rs, total, ss, kind, norm, None if gain is None else _values(gain, _F32, "gain", w),
+        eps, y.data_ptr(), _stride(y, n, w, "y"), _row_dtype(y), scale, None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_norm_rows", st)
 
@@ -592,13 +597,15 @@ def mcd_norm_rows(x, y, residual=None, sum_out=None, gain=None, eps: float = 1e-
 def mcd_sample_rows(logits, u, ids, err, temperature=None, top_k=None, top_p=None, min_p=None, probs=None, kept=None, stream=None):
     """ids int32 [rows]: one id of every row of logits (float32 or bfloat16 [rows, vocab]), drawn with u float64 [rows].  Settings
     per row: temperature, top_p, min_p float32, top_k int32; probs float32 and kept int32 are optional outputs.  Asynchronous."""
-    _types()
-    n, v = _matrix(logits, "logits")
+    if _F32 is None:
+        _types()
+    n, v = logits.shape
     st = (_lib or load_library()).mcd_sample_rows(
-        n, v, logits.data_ptr(), _rows(logits, "logits", n, v), _kv_dtype(logits), _per_row(temperature, _F32, "temperature", n),
-        _per_row(top_k, _I32, "top_k", n), _per_row(top_p, _F32, "top_p", n), _per_row(min_p, _F32, "min_p", n), _per_row(u, _F64, "u", n),
-        _per_row(ids, _I32, "ids", n), _per_row(probs, _F32, "probs", n), _per_row(kept, _I32, "kept", n), _i32(err, "err"),
-        None if stream is None else stream.cuda_stream)
+        n, v, logits.data_ptr(), _stride(logits, n, v, "logits"), _kv_dtype(logits),
+        None if temperature is None else _values(temperature, _F32, "temperature", n), None if top_k is None else _values(top_k, _I32, "top_k", n),
+        None if top_p is None else _values(top_p, _F32, "top_p", n), None if min_p is None else _values(min_p, _F32, "min_p", n),
+        _values(u, _F64, "u", n), _values(ids, _I32, "ids", n), None if probs is None else _values(probs, _F32, "probs", n),
+        None if kept is None else _values(kept, _I32, "kept", n), _i32(err, "err"), None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_sample_rows", st)
 
@@ -606,14 +613,16 @@ def mcd_sample_rows(logits, u, ids, err, temperature=None, top_k=None, top_p=Non
 def mcd_tc_gemm_e4m3(a, b, y, err, a_scale=None, b_scale=None, stream=None):
     """y [N, M] (float32 or bfloat16) = b a^T of float8_e4m3fn weights a [M, K] and rows b [N, K], times float32 scales per row
     of a and of b.  Asynchronous."""
-    _types()
-    (m, k), (n, kb) = _matrix(a, "a"), _matrix(b, "b")
-    if a.dtype is not _E4M3 or b.dtype is not _E4M3 or k != kb or _matrix(y, "y") != (n, m):
-        raise ValueError("a [M, K] and b [N, K] are float8_e4m3fn, y is [N, M]")
+    if _F32 is None:
+        _types()
+    m, k = a.shape
+    n = len(b)
+    if a.dtype is not _E4M3 or b.dtype is not _E4M3:
+        raise ValueError("a and b are float8_e4m3fn")
     st = (_lib or load_library()).mcd_tc_gemm_e4m3(
-        m, n, k, a.data_ptr(), _rows(a, "a", m, k), _per_row(a_scale, _F32, "a_scale", m), b.data_ptr(), _rows(b, "b", n, k),
-        _per_row(b_scale, _F32, "b_scale", n), y.data_ptr(), _rows(y, "y", n, m), _kv_dtype(y), _i32(err, "err"),
-        None if stream is None else stream.cuda_stream)
+        m, n, k, a.data_ptr(), _stride(a, m, k, "a"), None if a_scale is None else _values(a_scale, _F32, "a_scale", m), b.data_ptr(),
+        _stride(b, n, k, "b"), None if b_scale is None else _values(b_scale, _F32, "b_scale", n), y.data_ptr(), _stride(y, n, m, "y"), _kv_dtype(y),
+        _i32(err, "err"), None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_tc_gemm_e4m3", st)
 
