@@ -2,14 +2,16 @@
 //
 // The mathematics is in whole numbers: an id's weight is W = floor(2^31 exp32(logit / T - z_max)), and every filter is a cut of the
 // ranking (logit descending, id ascending): "the first k", "until the weights' sum reaches a target", "no weight below".
-// A cut is found without sorting, by a radix selection: a histogram (counts and sums of W) of the leading 8 bits of what is
-// left of the keys' range, the bin in which the target is crossed, then the next 8 bits in that bin.  The draw is the same
-// selection on ids in ascending order, its target a sum of weights.
+// A cut is found without sorting: a histogram (counts and sums of W) over 256 equal steps down from the maximum, the bin in which
+// the target is crossed, and of that bin's ids each one's sum of those before it (few ids; many are narrowed by histograms of
+// their keys first).  The draw is the same on ids in ascending order, its target a sum of weights.
 //
-// A cluster of CTAs takes a row.  It reads it for the maximum and, from the caches, once more: then ids within kNear of the
-// maximum (in units of T) go to a list in the first CTA's shared memory, and the sum of all weights is formed where top_p wants
-// it.  The list usually holds every id that the cuts leave, and the first CTA goes on alone with it; where it does not (or
-// nothing is cut), the whole cluster makes the selections' histograms from the row itself.
+// A cluster of CTAs takes a row and reads it for the maximum.  Then one of three ways:
+//   top_k up to the cluster's warps: so many ids are not below the least of the warps' maxima; what is not goes to a list in
+//     the first CTA's shared memory, and the first CTA goes on alone;
+//   top_k otherwise, top_p: the histogram is made from the row, by all CTAs; the ids of the bins down to the crossing one go to the list,
+//     as above; where they are too many, those of the crossing bin alone, and the draw is from the row;
+//   neither: the draw is from the row: sums of W of blocks of 256 ids, the block in which the target is crossed, the id.
 // Order never changes a result: whole numbers add up to the same sum.
 #include <cooperative_groups.h>
 
@@ -24,11 +26,12 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kList = 3584;            // ids of the list
-constexpr float kNear = 8.f;
+constexpr int kList = 3200;            // ids of the list
+constexpr int kFew = 128;              // ids whose order is found by comparing all with all
 constexpr int kMaxVocabRows = 1 << 18;
+constexpr int kBlocks = kMaxVocabRows / kMaxCluster / 256;      // blocks of 256 ids in a CTA's share
 
 struct SampleArgs {
   const void* logits;
@@ -49,6 +52,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
 struct Tally {
   unsigned long long mass;
@@ -56,20 +60,30 @@ struct Tally {
 };
 // What a CTA tells the others.
 struct Told {
-  float top;
+  float top, least;                    // its maximum, the least of its warps' maxima
   int bad;
-  Tally all, near;
+  uint32_t lo, hi;
+  Tally sum;
+};
+// A cut of the ranking: what is before it, itself included, is left.
+struct Cut {
+  uint32_t key, id;
+  Tally in;
 };
 
 struct Shared {
   uint32_t hist[3][256];               // counts, sums of the low 16 bits of W, of the others
   uint32_t key[kList], id[kList], w[kList];
-  uint32_t n_list;
-  Told told[3][kMaxCluster];           // of the maximum, of the lists, of the cuts
-  Tally red[kThreads / 32];
-  float fred[kThreads / 32];
+  uint32_t few_key[kFew], few_id[kFew], few_w[kFew];
+  unsigned long long block[kBlocks];
+  uint32_t n_list, n_few;
+  Told told[4][kMaxCluster];           // of the maximum, of sums, of extents
+  Tally red[kWarps];
+  float fred[kWarps];
+  uint32_t ured[2][kWarps];
   uint32_t bin;
   Tally above, at;
+  Cut cut;
 };
 
 __device__ __forceinline__ unsigned long long warp_sum(unsigned long long x) {
@@ -109,67 +123,62 @@ __device__ __forceinline__ void hist_add(Shared& sm, bool on, uint32_t bin, uint
   }
 }
 
-struct Pick {
-  uint32_t key;
-  Tally above, at;                     // of the larger keys, and of this one
+struct Level {
+  uint32_t bin;
+  Tally above, at;                     // of the bins above it, and of this one
+};
+// A histogram's sums, one bin a thread: thread t has bin 255 - t and what is above it.
+struct Bins {
+  Tally own, before;
 };
 
-// The largest key at which the running sum over descending keys (counts, or weights with by_mass) reaches `target` (at
-// least 1, at most the whole sum).  Keys are in [lo, lo + 2^bits); each(f) calls f(on, key, w) for the CTA's elements, warp by
-// warp.  With n > 1 the CTAs of the cluster do it together, each with its own elements.
+// each(f) calls f(on, bin, w) for the CTA's elements, warp by warp.  With n > 1 the CTAs of the cluster count together, each its
+// own elements, and have the same answer.
 template <class Each>
-__device__ __forceinline__ Pick pick(Shared& sm, int n, uint32_t lo, int bits, bool by_mass, unsigned long long target, Each each) {
+__device__ __forceinline__ Bins count_bins(Shared& sm, int n, Tally above, Each each) {
   cg::cluster_group cl = cg::this_cluster();
-  const int t = threadIdx.x;
-  Pick p{lo, {0ull, 0u}, {0ull, 0u}};
-  do {
-    const int shift = bits > 8 ? bits - 8 : 0;
-    for (int i = t; i < 3 * 256; i += kThreads) (&sm.hist[0][0])[i] = 0u;
-    __syncthreads();
-    const uint32_t base = p.key;
-    each([&](bool on, uint32_t key, uint32_t w) {
-      const uint32_t r = key - base;
-      on = on && key >= base && (bits >= 32 || r >> bits == 0);
-      hist_add(sm, on, on ? r >> shift : 0u, w);
-    });
-    if (n > 1) cl.sync();
-    else __syncthreads();
-    // bins in descending order, one a thread
-    Tally own{0ull, 0u};
-    if (t < 256) {
-      const int b = 255 - t;
-      for (int z = 0; z < n; ++z) {
-        const uint32_t* h = n > 1 ? cl.map_shared_rank(&sm.hist[0][0], z) : &sm.hist[0][0];
-        own.count += h[b];
-        own.mass += h[256 + b] + ((unsigned long long)h[512 + b] << 16);
-      }
+  const int t = threadIdx.x, lane = t & 31;
+  for (int i = t; i < 3 * 256; i += kThreads) (&sm.hist[0][0])[i] = 0u;
+  __syncthreads();
+  each([&](bool on, uint32_t bin, uint32_t w) { hist_add(sm, on, bin, w); });
+  if (n > 1) cl.sync();
+  else __syncthreads();
+  Bins b{{0ull, 0u}, above};
+  if (t < 256) {
+    for (int z = 0; z < n; ++z) {
+      const uint32_t* h = n > 1 ? cl.map_shared_rank(&sm.hist[0][0], z) : &sm.hist[0][0];
+      b.own.count += h[255 - t];
+      b.own.mass += h[511 - t] + ((unsigned long long)h[767 - t] << 16);
     }
-    Tally run = own;
-    const int lane = t & 31;
+    Tally run = b.own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const unsigned long long m = __shfl_up_sync(0xffffffffu, run.mass, d);
       const uint32_t c = __shfl_up_sync(0xffffffffu, run.count, d);
       if (lane >= d) run.mass += m, run.count += c;
     }
-    if (t < 256 && lane == 31) sm.red[t >> 5] = run;
-    __syncthreads();
-    if (t < 256) {
-      Tally from = p.above;
-      for (int i = 0; i < t >> 5; ++i) from.mass += sm.red[i].mass, from.count += sm.red[i].count;
-      const Tally before{from.mass + run.mass - own.mass, from.count + run.count - own.count};
-      const unsigned long long x = by_mass ? before.mass : before.count, y = by_mass ? own.mass : own.count;
-      if (x < target && target - x <= y) sm.bin = 255 - t, sm.above = before, sm.at = own;
-    }
-    if (n > 1) cl.sync();                              // (nobody clears what another still reads)
-    else __syncthreads();
-    p.key += sm.bin << shift;
-    p.above = sm.above;
-    p.at = sm.at;
-    bits = shift;
-    __syncthreads();
-  } while (bits > 0);
-  return p;
+    if (lane == 31) sm.red[t >> 5] = run;
+    b.before.mass += run.mass - b.own.mass, b.before.count += run.count - b.own.count;
+  }
+  if (n > 1) cl.sync();                                // (nobody clears what another still reads)
+  else __syncthreads();
+  for (int i = 0; i < (t >> 5) && t < 256; ++i) b.before.mass += sm.red[i].mass, b.before.count += sm.red[i].count;
+  return b;
+}
+// The bin at which the running sum (counts, or weights with by_mass) goes from below `target` to it or above.
+__device__ __forceinline__ Level crossing(Shared& sm, const Bins& b, bool by_mass, unsigned long long target) {
+  const unsigned long long x = by_mass ? b.before.mass : b.before.count, y = by_mass ? b.own.mass : b.own.count;
+  __syncthreads();
+  if (threadIdx.x < 256 && x < target && target - x <= y) sm.bin = 255 - threadIdx.x, sm.above = b.before, sm.at = b.own;
+  __syncthreads();
+  return {sm.bin, sm.above, sm.at};
+}
+// Sum of all bins.
+__device__ __forceinline__ Tally bins_sum(Shared& sm, const Bins& b) {
+  __syncthreads();
+  if (threadIdx.x == 255) sm.at = {b.before.mass + b.own.mass, b.before.count + b.own.count};
+  __syncthreads();
+  return sm.at;
 }
 
 template <class T>
@@ -179,29 +188,38 @@ __device__ __forceinline__ float logit_at(const float* row, int i) { return __ld
 template <>
 __device__ __forceinline__ float logit_at(const uint16_t* row, int i) { return bf16_bits_to_f32(__ldg(row + i)); }
 
-// f(on, id, logit) for the elements [lo, hi) of a row, lo a multiple of 8, warp by warp.
+// f(id, n, logits) for eight ids of a thread at a time, n of them in the share [lo, hi) (lo a multiple of 8), warp by warp: a
+// warp's eights are 256 ids in a row.  The next eight are on their way while these are looked at.
 template <class T, class F>
-__device__ __forceinline__ void each_logit(const T* row, int lo, int hi, F f) {
-  for (int i = lo + (threadIdx.x & ~31) * 8; i < hi; i += kThreads * 8) {
-    const int c = i + (threadIdx.x & 31) * 8;
-    float v[8];
+__device__ __forceinline__ void each_eight(const T* row, int lo, int hi, F f) {
+  const int lane = threadIdx.x & 31;
+  int i = lo + (threadIdx.x & ~31) * 8;
+  float next[8];
+  auto fetch = [&](int at) {
+    const int c = at + lane * 8;
     if (c + 8 <= hi) {
-      Vec8<T>::load(row + c, v);
+      Vec8<T>::load(row + c, next);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = c + e < hi ? logit_at(row, c + e) : 0.f;
+      for (int e = 0; e < 8; ++e) next[e] = c + e < hi ? logit_at(row, c + e) : 0.f;
     }
+  };
+  if (i < hi) fetch(i);
+  for (; i < hi; i += kThreads * 8) {
+    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f(c + e < hi, c + e, v[e]);
+    for (int e = 0; e < 8; ++e) v[e] = next[e];
+    if (i + kThreads * 8 < hi) fetch(i + kThreads * 8);
+    f(i + lane * 8, min(8, hi - i - lane * 8), v);
   }
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
   __shared__ Shared shared;
   Shared& sm = shared;
   cg::cluster_group cl = cg::this_cluster();
-  const int n = a.cluster, rank = n > 1 ? (int)cl.block_rank() : 0, t = threadIdx.x;
+  const int n = a.cluster, rank = n > 1 ? (int)cl.block_rank() : 0, t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const long long r = blockIdx.x / n;
   const int V = a.vocab, per = ((V + n - 1) / n + 7) / 8 * 8, lo = min(V, rank * per), hi = min(V, lo + per);
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
@@ -216,180 +234,415 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
               min_p = a.min_p ? __ldg(a.min_p + r) : 0.f;
   const int top_k = a.top_k ? __ldg(a.top_k + r) : 0;
   const double u = __ldg(a.u + r);
+  if (t == 0) sm.n_list = 0u;
 
   // ---- the largest logit
-  Told mine;
+  Told mine = {};
   {
-    float top = -INFINITY;
+    float most = -INFINITY;
     bool bad = false;
-    each_logit(row, lo, hi, [&](bool on, int, float x) {
-      if (!on) return;
-      top = fmaxf(top, x);
-      bad |= !(x <= 3.40282347e38f);                   // NaN or +inf
+    each_eight(row, lo, hi, [&](int, int left, const float (&v)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e >= left) continue;
+        most = fmaxf(most, v[e]);
+        bad |= !(v[e] <= 3.40282347e38f);              // NaN or +inf
+      }
     });
 #pragma unroll
-    for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-    if ((t & 31) == 0) sm.fred[t >> 5] = top;
-    if (t == 0) sm.n_list = 0u;
+    for (int w = 16; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+    if (lane == 0) sm.fred[warp] = most;
     mine.bad = __syncthreads_or(bad);
-    for (int i = 0; i < kThreads / 32; ++i) top = fmaxf(top, sm.fred[i]);
-    mine.top = top;
+    mine.top = -INFINITY, mine.least = INFINITY;
+    for (int i = 0; i < kWarps; ++i) mine.top = fmaxf(mine.top, sm.fred[i]), mine.least = fminf(mine.least, sm.fred[i]);
   }
+  // (every CTA's `mine` to all)
   auto tell = [&](int what) {
     if (t < n) *(n > 1 ? cl.map_shared_rank(&sm.told[what][rank], t) : &sm.told[what][0]) = mine;
     meet();
   };
-  mine.all = mine.near = {0ull, 0u};
   if (n > 1) cl.barrier_wait();                        // (the others have started)
   tell(0);
-  float top = -INFINITY;
+  float top = -INFINITY, least = INFINITY;
   bool bad = !(temp >= 0.f && temp <= 3.40282347e38f) || isnan(top_p) || isnan(min_p) || !(u >= 0. && u < 1.);
-  for (int z = 0; z < n; ++z) top = fmaxf(top, sm.told[0][z].top), bad |= sm.told[0][z].bad != 0;
+  for (int z = 0; z < n; ++z) top = fmaxf(top, sm.told[0][z].top), least = fminf(least, sm.told[0][z].least), bad |= sm.told[0][z].bad != 0;
   bad |= top == -INFINITY;
-  auto give = [&](int id, float prob, int kept) {
-    if (rank == 0 && t == 0) {
-      a.ids[r] = id;
-      if (a.probs) a.probs[r] = prob;
-      if (a.kept) a.kept[r] = kept;
-    }
+  auto give = [&](uint32_t id, unsigned long long w, Tally in) {
+    a.ids[r] = (int)id;
+    if (a.probs) a.probs[r] = (float)((double)w / (double)in.mass);
+    if (a.kept) a.kept[r] = (int)in.count;
   };
   if (bad) {                                           // (every CTA of the cluster alike, here and below)
-    if (rank == 0 && t == 0) atomicCAS(a.err, 0, (int)MCD_ERR_INVALID_ARG);
-    give(-1, 0.f, 0);
+    if (rank == 0 && t == 0) {
+      atomicCAS(a.err, 0, (int)MCD_ERR_INVALID_ARG);
+      give(0xffffffffu, 0ull, {1ull, 0u});
+    }
     return;
   }
+  const uint32_t key_top = key_of(top);
   const float z_top = __fdiv_rn(top, temp);
-  const bool has_k = top_k > 0 && top_k < V, has_p = top_p < 1.f;
+  const bool has_p = top_p < 1.f;
+  bool has_k = top_k > 0 && top_k < V;
   const bool greedy = temp == 0.f || !(fabsf(z_top) <= 3.40282347e38f) || top_k == 1 || top_p <= 0.f;
-  const float near = greedy ? top : top - kNear * temp;
   const uint32_t w_min = min_p > 0.f ? max(1u, (uint32_t)ceil((double)fminf(min_p, 1.f) * 2147483648.)) : 1u;
-  auto weight = [&](float x) {
-    if (greedy) return x >= top ? 1u : 0u;
-    return __float2uint_rd(__fmul_rn(exp32_cw(__fsub_rn(__fdiv_rn(x, temp), z_top)), 2147483648.f));
-  };
-  auto from_row = [&](auto key, auto want) {
-    return [=](auto f) {
-      each_logit(row, lo, hi, [&](bool on, int id, float x) {
-        const uint32_t k = key_of(x), w = on ? weight(x) : 0u;
-        f(on && w > 0u && want(k, (uint32_t)id, w), key(k, (uint32_t)id), w);
-      });
-    };
-  };
-  auto from_list = [&](auto key, auto want) {
-    return [=, &sm](auto f) {
+  auto weight = [&](float x) { return __float2uint_rd(__fmul_rn(exp32_cw(__fsub_rn(__fdiv_rn(x, temp), z_top)), 2147483648.f)); };
+
+  bool listed = false;
+  // f(on, key, id, weigh) for the CTA's share of the row, or (the first CTA alone) of the list, warp by warp
+  auto each = [&](auto f) {
+    if (listed) {
       const int count = (int)sm.n_list;
       for (int i = t & ~31; i < count; i += kThreads) {
-        const int j = i + (t & 31);
-        const bool on = j < count;
-        const uint32_t k = on ? sm.key[j] : 0u, id = on ? sm.id[j] : 0u, w = on ? sm.w[j] : 0u;
-        f(on && want(k, id, w), key(k, id), w);
+        const int j = min(i + lane, count - 1);
+        f(i + lane < count, sm.key[j], sm.id[j], [&] { return sm.w[j]; });
       }
-    };
+    } else {
+      each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = v[e];
+          f(e < left, key_of(x), (uint32_t)(id + e), [&] { return weight(x); });
+        }
+      });
+    }
   };
-
-  // ---- ids near the maximum to the first CTA's list; the sum of all weights where a cut or the draw needs it
-  const bool whole = !has_k && !greedy;
-  {
-    Tally all{0ull, 0u}, close{0ull, 0u};
+  // the least and largest of what `of` gives where it is not ~0
+  auto extent = [&](auto of) {
+    uint32_t from = 0xffffffffu, to = 0u;
+    each([&](bool on, uint32_t key, uint32_t id, auto) {
+      const uint32_t x = on ? of(key, id) : 0xffffffffu;
+      if (x != 0xffffffffu) from = min(from, x), to = max(to, x);
+    });
+    from = __reduce_min_sync(0xffffffffu, from), to = __reduce_max_sync(0xffffffffu, to);
+    __syncthreads();
+    if (lane == 0) sm.ured[0][warp] = from, sm.ured[1][warp] = to;
+    __syncthreads();
+    for (int i = 0; i < kWarps; ++i) from = min(from, sm.ured[0][i]), to = max(to, sm.ured[1][i]);
+    if (!listed && n > 1) {
+      mine.lo = from, mine.hi = to;
+      tell(2);
+      for (int z = 0; z < n; ++z) from = min(from, sm.told[2][z].lo), to = max(to, sm.told[2][z].hi);
+      meet();
+    }
+    return make_uint2(from, to);
+  };
+  if (greedy) {
+    const uint2 at = extent([&](uint32_t key, uint32_t id) { return key == key_top ? id : 0xffffffffu; });
+    if (rank == 0 && t == 0) give(at.x, 1ull, {1ull, 1u});
+    return;
+  }
+  // the row's ids that `want` takes and that have weight, to the list
+  auto gather = [&](auto want) {
     Shared& home = *(n > 1 ? cl.map_shared_rank(&sm, 0) : &sm);
-    each_logit(row, lo, hi, [&](bool on, int id, float x) {
-      uint32_t w = 0u;
-      if (on && (whole || x >= near)) w = weight(x);
-      all.mass += w;
-      const bool listed = on && x >= near && w > 0u;
-      const unsigned mask = __ballot_sync(0xffffffffu, listed);
-      if (!mask) return;
+    each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
+      uint32_t w[8];
+      int mine_n = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = e < left && want(v[e]) ? weight(v[e]) : 0u;
+        mine_n += w[e] > 0u;
+      }
+      if (!__any_sync(0xffffffffu, mine_n)) return;
+      int run = mine_n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, run, d);
+        if (lane >= d) run += x;
+      }
       uint32_t at = 0u;
-      if ((t & 31) == __ffs(mask) - 1) at = atomicAdd(&home.n_list, (uint32_t)__popc(mask));
-      at = __shfl_sync(0xffffffffu, at, __ffs(mask) - 1) + __popc(mask & ((1u << (t & 31)) - 1u));
-      if (listed) {
-        close.mass += w;
-        ++close.count;
-        if (at < (uint32_t)kList) home.key[at] = key_of(x), home.id[at] = (uint32_t)id, home.w[at] = w;
+      if (lane == 31) at = atomicAdd(&home.n_list, (uint32_t)run);
+      at = __shfl_sync(0xffffffffu, at, 31) + run - mine_n;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (w[e] == 0u) continue;
+        if (at < (uint32_t)kList) home.key[at] = key_of(v[e]), home.id[at] = (uint32_t)(id + e), home.w[at] = w[e];
+        ++at;
       }
     });
-    mine.all = block_sum(sm, all);
-    mine.near = block_sum(sm, close);
-  }
-  tell(1);
-  Tally all{0ull, 0u}, close{0ull, 0u};
-  for (int z = 0; z < n; ++z) {
-    all.mass += sm.told[1][z].all.mass;
-    close.mass += sm.told[1][z].near.mass, close.count += sm.told[1][z].near.count;
-  }
-  const bool listed = close.count <= (uint32_t)kList &&
-                      (greedy || (has_k ? close.count >= (uint32_t)top_k
-                                        : has_p && (double)close.mass >= ceil((double)top_p * (double)all.mass)));
-  const int id_bits = 32 - __clz(V);                   // (V - 1 - id < 2^id_bits)
-  auto by_key = [](uint32_t k, uint32_t) { return k; };
-  auto by_id = [V](uint32_t, uint32_t id) { return (uint32_t)(V - 1) - id; };
-
-  // The cuts and the draw, from the list (m = 1: the first CTA alone) or from the row (m = n).
-  auto finish = [&](int m, auto from) {
-    // counts and weights of what `want` takes, of all CTAs that take part
-    auto tally = [&](auto want) {
-      Tally x{0ull, 0u};
-      from(by_key, want)([&](bool on, uint32_t, uint32_t w) {
-        if (on) x.mass += w, ++x.count;
+    meet();
+  };
+  // narrows [at.x, at.y], a range of what `of` gives, to the one value where the running sum over descending values reaches the
+  // target; in: its sums, as far as they are known
+  auto narrow = [&](uint2 at, bool by_mass, unsigned long long target, Tally above, Tally in, uint32_t least_w, auto of) {
+    Level l{0u, above, in};
+    while (at.x != at.y) {
+      const int bits = 32 - __clz(at.y - at.x), shift = bits > 8 ? bits - 8 : 0;
+      const Bins b = count_bins(sm, listed ? 1 : n, l.above, [&](auto add) {
+        each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
+          const uint32_t x = on ? of(key, id) : 0xffffffffu;
+          on = x != 0xffffffffu && x >= at.x && x <= at.y;
+          const uint32_t w = on ? weigh() : 0u;
+          add(on && w >= least_w, on ? (x - at.x) >> shift : 0u, w);
+        });
       });
-      x = block_sum(sm, x);
-      if (m > 1) {
-        mine.all = x;
-        tell(2);
-        x = {0ull, 0u};
-        for (int z = 0; z < m; ++z) x.mass += sm.told[2][z].all.mass, x.count += sm.told[2][z].all.count;
-        meet();
-      }
-      return x;
+      l = crossing(sm, b, by_mass, target);
+      const uint32_t from = at.x + (l.bin << shift), to = min(at.y, from + ((1u << shift) - 1u));
+      at = from == to ? make_uint2(from, to) : extent([&](uint32_t key, uint32_t id) {
+        const uint32_t x = of(key, id);
+        return x >= from && x <= to ? x : 0xffffffffu;
+      });
+    }
+    l.bin = at.x;
+    return l;
+  };
+  auto from_id = [V](uint32_t id) { return (uint32_t)(V - 1) - id; };
+
+  // ---- cuts
+  Cut cut{0u, 0xffffffffu, {0ull, 0u}};
+  auto before_cut = [&](uint32_t key, uint32_t id) { return key > cut.key || (key == cut.key && id <= cut.id); };
+  // steps of the histograms: from the maximum down to where W is 0 (2^31 e^-21.5 < 1)
+  float scale = 255.f / (22.f * temp);
+  auto bin_of = [&](float x) { return 255u - (uint32_t)min(255, (int)((top - x) * scale)); };
+  auto key_bins = [&] {
+    return count_bins(sm, listed ? 1 : n, {0ull, 0u}, [&](auto add) {
+      each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
+        on = on && before_cut(key, id);
+        const uint32_t w = on ? weigh() : 0u;
+        add(on && w > 0u, on ? bin_of(logit_of(key)) : 0u, w);
+      });
+    });
+  };
+  // the few ids that `want` takes, to the short list
+  auto gather_few = [&](auto want) {
+    if (t == 0) sm.n_few = 0u;
+    __syncthreads();
+    each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
+      on = on && want(key, id);
+      const unsigned mask = __ballot_sync(0xffffffffu, on);
+      if (!mask) return;
+      uint32_t at = 0u;
+      if (lane == 0) at = atomicAdd(&sm.n_few, (uint32_t)__popc(mask));
+      at = __shfl_sync(0xffffffffu, at, 0) + __popc(mask & ((1u << lane) - 1u));
+      if (on && at < (uint32_t)kFew) sm.few_key[at] = key, sm.few_id[at] = id, sm.few_w[at] = weigh();
+    });
+    __syncthreads();
+    return min((int)sm.n_few, kFew);
+  };
+  // the cut in bin l.bin
+  auto cut_in = [&](const Level l, bool by_mass, unsigned long long target) {
+    const Cut old = cut;
+    auto member = [&](uint32_t key, uint32_t id) {
+      return (key > old.key || (key == old.key && id <= old.id)) && bin_of(logit_of(key)) == l.bin;
     };
-    auto any = [](uint32_t, uint32_t, uint32_t) { return true; };
-    uint32_t cut = 0u, last = 0xffffffffu;             // larger keys are left, and of this one the ids up to `last`
-    unsigned long long mass = all.mass;
-    const uint32_t key_top = key_of(top);
-    bool ties = false;
-    uint32_t n_ties = 0u;
-    if (greedy) {
-      cut = key_top, n_ties = 1u, ties = true;
-    } else {
-      if (has_k) {
-        // (ids without weight are behind all others)
-        const Tally some = listed ? close : tally(any);
-        mass = some.mass;
-        if ((uint32_t)top_k < some.count) {
-          const Pick p = pick(sm, m, 0u, 32, false, (unsigned long long)top_k, from(by_key, any));
-          cut = p.key;
-          n_ties = (uint32_t)top_k - p.above.count;
-          ties = n_ties < p.at.count;
-          mass = p.above.mass + p.at.mass / p.at.count * n_ties;
+    if (listed && l.at.count <= (uint32_t)kFew) {
+      const int few = gather_few(member);
+      if (t < few) {
+        const uint32_t key = sm.few_key[t], id = sm.few_id[t], w = sm.few_w[t];
+        Tally b = l.above;
+#pragma unroll 4
+        for (int j = 0; j < few; ++j) {
+          const uint32_t k = sm.few_key[j];
+          if (k > key || (k == key && sm.few_id[j] < id)) b.mass += sm.few_w[j], ++b.count;
+        }
+        const unsigned long long x = by_mass ? b.mass : b.count;
+        if (x < target && target - x <= (by_mass ? w : 1u)) sm.cut = {key, id, {b.mass + w, b.count + 1u}};
+      }
+      __syncthreads();
+      cut = sm.cut;
+      __syncthreads();
+      return;
+    }
+    auto of = [&](uint32_t key, uint32_t id) { return member(key, id) ? key : 0xffffffffu; };
+    const Level p = narrow(extent(of), by_mass, target, l.above, l.at, 1u, of);
+    // (p.at can hold ids behind the old cut: it does not tell the weight, and of the count only that there are no more)
+    const unsigned long long one = weight(logit_of(p.bin));
+    const uint32_t ties = (uint32_t)(by_mass ? (target - p.above.mass + one - 1) / one : target - p.above.count);
+    cut.key = p.bin;
+    if (ties < p.at.count) {
+      auto tie = [&](uint32_t key, uint32_t id) { return key == cut.key && (key > old.key || id <= old.id) ? from_id(id) : 0xffffffffu; };
+      cut.id = from_id(narrow(extent(tie), false, ties, {0ull, 0u}, {0ull, 0u}, 1u, tie).bin);
+    } else if (cut.key > old.key) {
+      cut.id = 0xffffffffu;
+    }
+    cut.in = {p.above.mass + one * ties, p.above.count + ties};
+  };
+  // (top_p < 1 and a mass below 2^50: the product is at most the mass)
+  auto need_of = [&](unsigned long long mass) { return min(max(1ull, (unsigned long long)ceil((double)top_p * (double)mass)), mass); };
+
+  bool p_done = false;
+  if (has_k && top_k <= n * kWarps) {
+    // a rounded quotient can put an id of weight below the point where none should have any: 1e-6 of the logits covers it
+    const float near = fmaxf(least, top - 22.f * temp - fabsf(top) * 1e-6f);
+    gather([&](float x) { return x >= near; });
+    cut.in.count = *(n > 1 ? cl.map_shared_rank(&sm.n_list, 0) : &sm.n_list);
+    listed = cut.in.count <= (uint32_t)kList;
+    meet();                                            // (read by all)
+    if (listed) {
+      if (rank > 0) return;
+      const float span = top - near;
+      scale = span > 0.f ? 255.f / span : 0.f;
+      const Bins b = key_bins();
+      cut.in = bins_sum(sm, b);
+      if ((uint32_t)top_k < cut.in.count) cut_in(crossing(sm, b, false, top_k), false, top_k);
+    } else if (rank == 0 && t == 0) {
+      sm.n_list = 0u;
+    }
+  }
+  if ((has_k || has_p) && !listed) {
+    const Bins b = key_bins();
+    cut.in = bins_sum(sm, b);
+    has_k = has_k && (uint32_t)top_k < cut.in.count;
+    unsigned long long target = has_k ? (unsigned long long)top_k : need_of(cut.in.mass);
+    // (a bin's ids to the list, or all down to it: the first CTA alone finds the cut and, in the first case, tells the others)
+    auto find = [&](const Level l, bool by_mass) {
+      const bool all = l.above.count + l.at.count <= (uint32_t)kList;
+      if (!all && l.at.count > (uint32_t)kList) {
+        cut_in(l, by_mass, target);
+        return;
+      }
+      gather([&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      listed = all;
+      if (rank > 0 && all) return;
+      if (rank == 0) {
+        listed = true;
+        cut_in(l, by_mass, target);
+        listed = all;
+      }
+      if (all) return;
+      if (rank == 0) {
+        if (t == 0) sm.n_list = 0u;
+        if (t < n) *(n > 1 ? cl.map_shared_rank(&sm.cut, t) : &sm.cut) = cut;
+      }
+      meet();
+      cut = sm.cut;
+      meet();
+    };
+    if (has_k || has_p) {
+      find(crossing(sm, b, !has_k, target), !has_k);
+      if (listed && rank > 0) return;
+      p_done = !has_k;
+      if (has_k && has_p && !listed) {
+        target = need_of(cut.in.mass);
+        find(crossing(sm, b, true, target), true);
+        if (listed && rank > 0) return;
+        p_done = true;
+      }
+    }
+  }
+
+  // ---- the draw
+  if (!listed) {
+    // from the row: blocks of 256 ids
+    Tally x{0ull, 0u};
+    int i = warp;
+    each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
+      Tally y{0ull, 0u};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e >= left || !before_cut(key_of(v[e]), (uint32_t)(id + e))) continue;
+        const uint32_t w = weight(v[e]);
+        if (w >= w_min) y.mass += w, ++y.count;
+      }
+      y.mass = warp_sum(y.mass);
+      if (lane == 0) sm.block[i] = y.mass, x.mass += y.mass;
+      x.count += y.count;
+      i += kWarps;
+    });
+    mine.sum = block_sum(sm, x);
+    tell(1);
+    Tally in{0ull, 0u};
+    unsigned long long ahead = 0ull;
+    for (int z = 0; z < n; ++z) {
+      if (z < rank) ahead += sm.told[1][z].sum.mass;
+      in.mass += sm.told[1][z].sum.mass, in.count += sm.told[1][z].sum.count;
+    }
+    const unsigned long long drawn = min((unsigned long long)floor(u * (double)in.mass), in.mass - 1);
+    if (drawn < ahead || drawn - ahead >= mine.sum.mass || warp > 0) return;
+    unsigned long long rest = drawn - ahead;           // (in this CTA's share)
+    const int blocks = (hi - lo + 255) / 256;
+    int from = 0;
+    for (; from < blocks; from += 32) {                // the block, 32 at a time
+      const unsigned long long own = from + lane < blocks ? sm.block[from + lane] : 0ull;
+      unsigned long long run = own;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned long long y = __shfl_up_sync(0xffffffffu, run, d);
+        if (lane >= d) run += y;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, rest < run);
+      if (hit) {
+        const int f = __ffs(hit) - 1;
+        rest -= __shfl_sync(0xffffffffu, run - own, f);
+        from += f;
+        break;
+      }
+      rest -= __shfl_sync(0xffffffffu, run, 31);
+    }
+    const int id = lo + from * 256 + lane * 8;
+    uint32_t w[8];
+    unsigned long long own = 0ull;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = 0u;
+      if (id + e >= hi) continue;
+      const float x = logit_at(row, id + e);
+      if (before_cut(key_of(x), (uint32_t)(id + e))) w[e] = weight(x);
+      if (w[e] < w_min) w[e] = 0u;
+      own += w[e];
+    }
+    unsigned long long run = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, run, d);
+      if (lane >= d) run += y;
+    }
+    unsigned long long at = run - own;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (w[e] > 0u && at <= rest && rest < at + w[e]) give((uint32_t)(id + e), w[e], in);
+      at += w[e];
+    }
+    return;
+  }
+  // from the list (the first CTA alone)
+  if (has_p && !p_done && cut.in.count > (uint32_t)kFew) {
+    const unsigned long long need = need_of(cut.in.mass);
+    const Bins b = key_bins();
+    cut_in(crossing(sm, b, true, need), true, need);
+    p_done = true;
+  }
+  if (cut.in.count <= (uint32_t)kFew) {
+    const int few = gather_few(before_cut);
+    const unsigned long long need = has_p && !p_done ? need_of(cut.in.mass) : ~0ull;
+    uint32_t key = 0u, id = 0u, w = 0u;
+    if (t < few) {
+      key = sm.few_key[t], id = sm.few_id[t], w = sm.few_w[t];
+      unsigned long long b = 0ull;
+      if (need != ~0ull) {
+#pragma unroll 4
+        for (int j = 0; j < few; ++j) {
+          const uint32_t k = sm.few_key[j];
+          if (k > key || (k == key && sm.few_id[j] < id)) b += sm.few_w[j];
         }
       }
-      if (has_p) {
-        // (with top_p < 1 and mass < 2^50, the product is at most mass)
-        const unsigned long long need = max(1ull, (unsigned long long)ceil((double)top_p * (double)mass));
-        const uint32_t c = cut;
-        const Pick p = pick(sm, m, 0u, 32, true, min(need, mass), from(by_key, [c](uint32_t k, uint32_t, uint32_t) { return k >= c; }));
-        const unsigned long long one = p.at.mass / p.at.count;
-        cut = p.key;
-        n_ties = (uint32_t)((min(need, mass) - p.above.mass + one - 1) / one);
-        ties = n_ties < p.at.count;
-      }
+      if (b >= need || w < w_min) w = 0u;
     }
-    if (ties) {
-      const uint32_t c = cut;
-      const Pick p = pick(sm, m, 0u, id_bits, false, n_ties, from(by_id, [c](uint32_t k, uint32_t, uint32_t) { return k == c; }));
-      last = (uint32_t)(V - 1) - p.key;
+    __syncthreads();
+    if (t < few) sm.few_w[t] = w;
+    const Tally in = block_sum(sm, {w, w > 0u});
+    const unsigned long long drawn = min((unsigned long long)floor(u * (double)in.mass), in.mass - 1);
+    if (w > 0u) {
+      unsigned long long b = 0ull;
+#pragma unroll 4
+      for (int j = 0; j < few; ++j)
+        if (sm.few_id[j] < id) b += sm.few_w[j];
+      if (b <= drawn && drawn < b + w) give(id, w, in);
     }
-    auto left = [=](uint32_t k, uint32_t id, uint32_t w) { return (k > cut || (k == cut && id <= last)) && w >= (greedy ? 0u : w_min); };
-    const Tally x = tally(left);
-    const unsigned long long drawn = min((unsigned long long)floor(u * (double)x.mass), x.mass - 1);
-    const Pick p = pick(sm, m, 0u, id_bits, true, drawn + 1, from(by_id, left));
-    give(V - 1 - (int)p.key, (float)((double)p.at.mass / (double)x.mass), (int)x.count);
-  };
-  if (listed) {
-    if (rank == 0) finish(1, from_list);
-  } else {
-    finish(n, from_row);
+    return;
   }
+  Tally in = cut.in;
+  if (w_min > 1u) {
+    Tally x{0ull, 0u};
+    each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
+      const uint32_t w = on && before_cut(key, id) ? weigh() : 0u;
+      if (w >= w_min) x.mass += w, ++x.count;
+    });
+    in = block_sum(sm, x);
+  }
+  const unsigned long long drawn = min((unsigned long long)floor(u * (double)in.mass), in.mass - 1);
+  auto of = [&](uint32_t key, uint32_t id) { return before_cut(key, id) ? from_id(id) : 0xffffffffu; };
+  const Level p = narrow(extent(of), true, drawn + 1, {0ull, 0u}, in, w_min, of);
+  if (t == 0) give(from_id(p.bin), p.at.mass, in);
 }
 
 // CTAs of a row: enough that each has kSlice ids at most.
