@@ -7,8 +7,8 @@
 // their keys first).  The draw is the same on ids in ascending order, its target a sum of weights.
 //
 // A cluster of CTAs takes a row and reads it for the maximum.  Then one of three ways:
-//   top_k up to the cluster's warps: so many ids are not below the least of the warps' maxima; what is not goes to a list in
-//     the first CTA's shared memory, and the first CTA goes on alone;
+//   top_k up to the cluster's half warps: so many ids are not below the least of the half warps' maxima; what is not goes to a
+//     list in the first CTA's shared memory, and the first CTA goes on alone;
 //   top_k otherwise, top_p: the histogram is made from the row, by all CTAs; the ids of the bins down to the crossing one go to the list,
 //     as above; where they are too many, those of the crossing bin alone, and the draw is from the row;
 //   neither: the draw is from the row: sums of W of blocks of 256 ids, the block in which the target is crossed, the id.
@@ -17,6 +17,7 @@
 
 #include <cmath>
 
+#include "mcd_cache.cuh"
 #include "mcd_rows.cuh"
 #include "mcd_sampler.cuh"
 
@@ -26,7 +27,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kGroups = 2 * kWarps;    // halves of warps, whose maxima bound the largest ids
 constexpr int kMaxCluster = 8;
 constexpr int kList = 3200;            // ids of the list
 constexpr int kFew = 128;              // ids whose order is found by comparing all with all
@@ -60,7 +62,7 @@ struct Tally {
 };
 // What a CTA tells the others.
 struct Told {
-  float top, least;                    // its maximum, the least of its warps' maxima
+  float top, least;                    // its maximum, the least of its groups' maxima
   int bad;
   uint32_t lo, hi;
   Tally sum;
@@ -74,12 +76,12 @@ struct Cut {
 struct Shared {
   uint32_t hist[3][256];               // counts, sums of the low 16 bits of W, of the others
   uint32_t key[kList], id[kList], w[kList];
-  uint32_t few_key[kFew], few_id[kFew], few_w[kFew];
+  uint4 few[kFew];                     // key, id, W
   unsigned long long block[kBlocks];
   uint32_t n_list, n_few;
   Told told[4][kMaxCluster];           // of the maximum, of sums, of extents
   Tally red[kWarps];
-  float fred[kWarps];
+  float fred[kGroups];
   uint32_t ured[2][kWarps];
   uint32_t bin;
   Tally above, at;
@@ -90,6 +92,11 @@ __device__ __forceinline__ unsigned long long warp_sum(unsigned long long x) {
 #pragma unroll
   for (int w = 16; w; w >>= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
   return x;
+}
+// The same of numbers below 2^36.
+__device__ __forceinline__ unsigned long long warp_sum36(unsigned long long x) {
+  const uint32_t lo = __reduce_add_sync(0xffffffffu, (uint32_t)x & 0x3ffffu), hi = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 18));
+  return lo + ((unsigned long long)hi << 18);
 }
 // Sum over the CTA, in every thread.
 __device__ __forceinline__ Tally block_sum(Shared& sm, Tally t) {
@@ -104,6 +111,12 @@ __device__ __forceinline__ Tally block_sum(Shared& sm, Tally t) {
   return t;
 }
 
+__device__ __forceinline__ void hist_add_one(Shared& sm, bool on, uint32_t bin, uint32_t w) {
+  if (!on) return;
+  atomicAdd(&sm.hist[0][bin], 1u);
+  atomicAdd(&sm.hist[1][bin], w & 0xffffu);
+  atomicAdd(&sm.hist[2][bin], w >> 16);
+}
 // One element to the histogram (all lanes of the warp call it).  Lanes of one bin, as neighbours in id order are, add up first.
 __device__ __forceinline__ void hist_add(Shared& sm, bool on, uint32_t bin, uint32_t w) {
   const unsigned mask = __ballot_sync(0xffffffffu, on);
@@ -116,12 +129,77 @@ __device__ __forceinline__ void hist_add(Shared& sm, bool on, uint32_t bin, uint
       atomicAdd(&sm.hist[1][first], lo);
       atomicAdd(&sm.hist[2][first], hi);
     }
-  } else if (on) {
-    atomicAdd(&sm.hist[0][bin], 1u);
-    atomicAdd(&sm.hist[1][bin], w & 0xffffu);
-    atomicAdd(&sm.hist[2][bin], w >> 16);
+  } else {
+    hist_add_one(sm, on, bin, w);
   }
 }
+
+// W of a logit: its quotient with T, the exponential of the difference from the maximum's, in the steps that define them.  Eight of
+// a thread at a time, two an instruction, without branches.  The quotient is Markstein's (IBM J. Res. Dev. 34, 1990): from the
+// correctly rounded 1 / T two corrections by the exact remainder give the correctly rounded quotient while nothing under- or
+// overflows; elsewhere (`plain` false, or a logit far from 1) it is divided.  Rounding to a whole number is by adding 1.5 * 2^23, whose
+// last bits then are that number.
+struct Weigh {
+  float temp, inverse, z_top;
+  bool plain;
+  __device__ __forceinline__ uint32_t operator()(float x) const {
+    return __float2uint_rd(__fmul_rn(exp32_cw(__fsub_rn(__fdiv_rn(x, temp), z_top)), 2147483648.f));
+  }
+  __device__ __forceinline__ void eight(const float (&v)[8], uint32_t (&w)[8]) const {
+    using namespace paged;
+    auto both = [](float x) { return pack2(x, x); };
+    uint64_t z[4];
+    bool near = plain;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) near &= ((__float_as_uint(v[e]) & 0x7fffffffu) - 0x27000000u) < 0x30000000u;      // 2^-49 .. 2^47
+    if (__all_sync(__activemask(), near)) {
+      const uint64_t inv = both(inverse), minus = both(-temp);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t x = pack2(v[2 * e], v[2 * e + 1]), q0 = mul2(x, inv), q1 = fma2(fma2(q0, minus, x), inv, q0);
+        z[e] = fma2(fma2(q1, minus, x), inv, q1);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = pack2(__fdiv_rn(v[2 * e], temp), __fdiv_rn(v[2 * e + 1], temp));
+    }
+    // (one at a time: ptxas makes a mul.rn.f32x2 and the add.rn.f32x2 that takes it one operation, rounded once)
+    auto plus = [](uint64_t a, float b) {
+      float x, y;
+      unpack2(a, x, y);
+      return pack2(__fadd_rn(x, b), __fadd_rn(y, b));
+    };
+    auto sum = [](uint64_t a, uint64_t b) {
+      float x, y, u, v;
+      unpack2(a, x, y);
+      unpack2(b, u, v);
+      return pack2(__fadd_rn(x, u), __fadd_rn(y, v));
+    };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float d[2], y[2], p[2];
+      unpack2(add2(z[e], both(-z_top)), d[0], d[1]);
+      const uint64_t x = pack2(fmaxf(d[0], -87.f), fmaxf(d[1], -87.f));
+      const uint64_t t = plus(mul2(x, both(__int_as_float(0x3fb8aa3b))), 12582912.f), n = plus(t, -12582912.f);
+      const uint64_t r = sum(sum(x, mul2(n, both(-__int_as_float(0x3f318000)))), mul2(n, both(-__int_as_float(0xb95e8083))));
+      uint64_t s = both(__int_as_float(0x39500d01));
+      s = plus(mul2(s, r), __int_as_float(0x3ab60b61));
+      s = plus(mul2(s, r), __int_as_float(0x3c088889));
+      s = plus(mul2(s, r), __int_as_float(0x3d2aaaab));
+      s = plus(mul2(s, r), __int_as_float(0x3e2aaaab));
+      s = plus(mul2(s, r), 0.5f);
+      s = plus(mul2(s, r), 1.f);
+      s = plus(mul2(s, r), 1.f);
+      unpack2(t, y[0], y[1]);
+      unpack2(s, p[0], p[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {                    // (times 2^(n + 31): powers of two)
+        const uint32_t u = __float2uint_rd(__fmul_rn(p[i], __uint_as_float((__float_as_uint(y[i]) << 23) + (158u << 23))));
+        w[2 * e + i] = d[i] < -87.f ? 0u : u;
+      }
+    }
+  }
+};
 
 struct Level {
   uint32_t bin;
@@ -188,34 +266,68 @@ __device__ __forceinline__ float logit_at(const float* row, int i) { return __ld
 template <>
 __device__ __forceinline__ float logit_at(const uint16_t* row, int i) { return bf16_bits_to_f32(__ldg(row + i)); }
 
+// Eight logits as they lie.
+template <class T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+  static constexpr int kAhead = 2;
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ void set(const float (&v)[8]) { a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
+};
+template <>
+struct Raw8<uint16_t> {
+  static constexpr int kAhead = 4;
+  uint4 a;
+  __device__ __forceinline__ void load(const uint16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    a = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo_f32(w[i]), v[2 * i + 1] = bf16_hi_f32(w[i]);
+  }
+};
 // f(id, n, logits) for eight ids of a thread at a time, n of them in the share [lo, hi) (lo a multiple of 8), warp by warp: a
-// warp's eights are 256 ids in a row.  The next eight are on their way while these are looked at.
+// warp's eights are 256 ids in a row.  The next ones are on their way while these are looked at.
 template <class T, class F>
 __device__ __forceinline__ void each_eight(const T* row, int lo, int hi, F f) {
+  constexpr int kAhead = Raw8<T>::kAhead, kStep = kThreads * 8;
   const int lane = threadIdx.x & 31;
   int i = lo + (threadIdx.x & ~31) * 8;
-  float next[8];
-  auto fetch = [&](int at) {
+  Raw8<T> next[kAhead];
+  auto fetch = [&](int at, Raw8<T>& to) {
     const int c = at + lane * 8;
     if (c + 8 <= hi) {
-      Vec8<T>::load(row + c, next);
+      to.load(row + c);
     } else {
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) next[e] = c + e < hi ? logit_at(row, c + e) : 0.f;
+      for (int e = 0; e < 8; ++e) v[e] = c + e < hi ? logit_at(row, c + e) : 0.f;
+      to.set(v);
     }
   };
-  if (i < hi) fetch(i);
-  for (; i < hi; i += kThreads * 8) {
-    float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = next[e];
-    if (i + kThreads * 8 < hi) fetch(i + kThreads * 8);
+  for (int k = 0; k < kAhead; ++k)
+    if (i + k * kStep < hi) fetch(i + k * kStep, next[k]);
+#pragma unroll 1
+  for (; i < hi; i += kStep) {
+    float v[8];
+    next[0].get(v);
+#pragma unroll
+    for (int k = 0; k + 1 < kAhead; ++k) next[k] = next[k + 1];
+    if (i + kAhead * kStep < hi) fetch(i + kAhead * kStep, next[kAhead - 1]);
     f(i + lane * 8, min(8, hi - i - lane * 8), v);
   }
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a) {
   __shared__ Shared shared;
   Shared& sm = shared;
   cg::cluster_group cl = cg::this_cluster();
@@ -234,7 +346,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
               min_p = a.min_p ? __ldg(a.min_p + r) : 0.f;
   const int top_k = a.top_k ? __ldg(a.top_k + r) : 0;
   const double u = __ldg(a.u + r);
-  if (t == 0) sm.n_list = 0u;
 
   // ---- the largest logit
   Told mine = {};
@@ -250,11 +361,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
       }
     });
 #pragma unroll
-    for (int w = 16; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
-    if (lane == 0) sm.fred[warp] = most;
+    for (int w = 8; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+    if ((lane & 15) == 0) sm.fred[t >> 4] = most;
     mine.bad = __syncthreads_or(bad);
     mine.top = -INFINITY, mine.least = INFINITY;
-    for (int i = 0; i < kWarps; ++i) mine.top = fmaxf(mine.top, sm.fred[i]), mine.least = fminf(mine.least, sm.fred[i]);
+    for (int i = 0; i < kGroups; ++i) mine.top = fmaxf(mine.top, sm.fred[i]), mine.least = fminf(mine.least, sm.fred[i]);
   }
   // (every CTA's `mine` to all)
   auto tell = [&](int what) {
@@ -285,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   bool has_k = top_k > 0 && top_k < V;
   const bool greedy = temp == 0.f || !(fabsf(z_top) <= 3.40282347e38f) || top_k == 1 || top_p <= 0.f;
   const uint32_t w_min = min_p > 0.f ? max(1u, (uint32_t)ceil((double)fminf(min_p, 1.f) * 2147483648.)) : 1u;
-  auto weight = [&](float x) { return __float2uint_rd(__fmul_rn(exp32_cw(__fsub_rn(__fdiv_rn(x, temp), z_top)), 2147483648.f)); };
+  const Weigh weight{temp, __fdiv_rn(1.f, temp), z_top, temp > 1e-15f && temp < 1e15f};
 
   bool listed = false;
   // f(on, key, id, weigh) for the CTA's share of the row, or (the first CTA alone) of the list, warp by warp
@@ -294,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
       const int count = (int)sm.n_list;
       for (int i = t & ~31; i < count; i += kThreads) {
         const int j = min(i + lane, count - 1);
-        f(i + lane < count, sm.key[j], sm.id[j], [&] { return sm.w[j]; });
+        f(i + lane < count && sm.w[j] > 0u, sm.key[j], sm.id[j], [&] { return sm.w[j]; });
       }
     } else {
       each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
@@ -331,35 +442,60 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     if (rank == 0 && t == 0) give(at.x, 1ull, {1ull, 1u});
     return;
   }
-  // the row's ids that `want` takes and that have weight, to the list
+  // the row's ids that `want` takes (some may have no weight): to each CTA's list, and if there are no more than it holds, all to the
+  // first one's; how many there are
   auto gather = [&](auto want) {
-    Shared& home = *(n > 1 ? cl.map_shared_rank(&sm, 0) : &sm);
+    if (t == 0) sm.n_list = 0u;
+    __syncthreads();
     each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
-      uint32_t w[8];
-      int mine_n = 0;
+      uint32_t on = 0u;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        w[e] = e < left && want(v[e]) ? weight(v[e]) : 0u;
-        mine_n += w[e] > 0u;
-      }
-      if (!__any_sync(0xffffffffu, mine_n)) return;
-      int run = mine_n;
+      for (int e = 0; e < 8; ++e) on |= (uint32_t)(e < left && want(v[e])) << e;
+      // (few of a warp's ids, as a rule: one of a lane at a time)
+      for (unsigned mask; (mask = __ballot_sync(0xffffffffu, on != 0u)) != 0u; on &= on - 1u) {
+        uint32_t at = 0u;
+        if (lane == 0) at = atomicAdd(&sm.n_list, (uint32_t)__popc(mask));
+        at = __shfl_sync(0xffffffffu, at, 0) + __popc(mask & ((1u << lane) - 1u));
+        const int first = __ffs(on) - 1;
+        float x = v[0];
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, run, d);
-        if (lane >= d) run += x;
-      }
-      uint32_t at = 0u;
-      if (lane == 31) at = atomicAdd(&home.n_list, (uint32_t)run);
-      at = __shfl_sync(0xffffffffu, at, 31) + run - mine_n;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (w[e] == 0u) continue;
-        if (at < (uint32_t)kList) home.key[at] = key_of(v[e]), home.id[at] = (uint32_t)(id + e), home.w[at] = w[e];
-        ++at;
+        for (int e = 1; e < 8; ++e) x = e == first ? v[e] : x;
+        if (on != 0u && at < (uint32_t)kList) sm.key[at] = key_of(x), sm.id[at] = (uint32_t)(id + first);
       }
     });
-    meet();
+    __syncthreads();
+    // their weights
+    const int count = min((int)sm.n_list, kList);
+    for (int i = t * 8; i < count; i += kThreads * 8) {
+      float v[8];
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = i + e < count ? logit_of(sm.key[i + e]) : 0.f;
+      weight.eight(v, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (i + e < count) sm.w[i + e] = w[e];
+    }
+    __syncthreads();
+    if (n == 1) return sm.n_list;
+    mine.lo = sm.n_list;
+    tell(3);
+    uint32_t sum = 0u;
+    for (int z = 0; z < n; ++z) sum += sm.told[3][z].lo;
+    if (rank == 0 && sum <= (uint32_t)kList) {
+      static_assert(kWarps >= kMaxCluster, "a warp fetches a list");
+      if (warp > 0 && warp < n) {
+        uint32_t from = 0u;
+        for (int z = 0; z < warp; ++z) from += sm.told[3][z].lo;
+        const uint32_t count = sm.told[3][warp].lo;
+        const Shared& other = *cl.map_shared_rank(&sm, warp);
+#pragma unroll 4
+        for (uint32_t i = lane; i < count; i += 32) sm.key[from + i] = other.key[i], sm.id[from + i] = other.id[i], sm.w[from + i] = other.w[i];
+      }
+      if (t == 0) sm.n_list = sum;
+    }
+    cl.sync();                                         // (the lists have been read)
+    return sum;
   };
   // narrows [at.x, at.y], a range of what `of` gives, to the one value where the running sum over descending values reaches the
   // target; in: its sums, as far as they are known
@@ -390,17 +526,43 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   // ---- cuts
   Cut cut{0u, 0xffffffffu, {0ull, 0u}};
   auto before_cut = [&](uint32_t key, uint32_t id) { return key > cut.key || (key == cut.key && id <= cut.id); };
-  // steps of the histograms: from the maximum down to where W is 0 (2^31 e^-21.5 < 1)
+  // steps of the histograms: from the maximum down to kNear T below it, to 22 T where W is 0 (2^31 e^-21.5 < 1), or to the list's end
+  constexpr float kNear = 8.f;
   float scale = 255.f / (22.f * temp);
   auto bin_of = [&](float x) { return 255u - (uint32_t)min(255, (int)((top - x) * scale)); };
-  auto key_bins = [&] {
-    return count_bins(sm, listed ? 1 : n, {0ull, 0u}, [&](auto add) {
-      each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
-        on = on && before_cut(key, id);
-        const uint32_t w = on ? weigh() : 0u;
-        add(on && w > 0u, on ? bin_of(logit_of(key)) : 0u, w);
-      });
+  // (ids below `low` are counted in the last bin's place: `rest` is their sum)
+  auto key_bins = [&](float low, Tally& rest) {
+    Tally out{0ull, 0u};
+    const Bins b = count_bins(sm, listed ? 1 : n, {0ull, 0u}, [&](auto) {
+      if (listed) {
+        each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
+          hist_add_one(sm, on && before_cut(key, id), bin_of(logit_of(key)), weigh());
+        });
+      } else {
+        each_eight(row, lo, hi, [&](int, int left, const float (&v)[8]) {
+          uint32_t w[8];
+          weight.eight(v, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool on = e < left && w[e] > 0u, far = on && v[e] < low;
+            out.mass += far ? w[e] : 0u, out.count += far;
+            hist_add_one(sm, on && !far, bin_of(v[e]), w[e]);
+          }
+        });
+      }
     });
+    rest = out;
+    if (!listed) {
+      rest = block_sum(sm, out);
+      if (n > 1) {
+        mine.sum = rest;
+        tell(1);
+        rest = {0ull, 0u};
+        for (int z = 0; z < n; ++z) rest.mass += sm.told[1][z].sum.mass, rest.count += sm.told[1][z].sum.count;
+        meet();
+      }
+    }
+    return b;
   };
   // the few ids that `want` takes, to the short list
   auto gather_few = [&](auto want) {
@@ -413,26 +575,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
       uint32_t at = 0u;
       if (lane == 0) at = atomicAdd(&sm.n_few, (uint32_t)__popc(mask));
       at = __shfl_sync(0xffffffffu, at, 0) + __popc(mask & ((1u << lane) - 1u));
-      if (on && at < (uint32_t)kFew) sm.few_key[at] = key, sm.few_id[at] = id, sm.few_w[at] = weigh();
+      if (on && at < (uint32_t)kFew) sm.few[at] = make_uint4(key, id, weigh(), 0u);
     });
     __syncthreads();
     return min((int)sm.n_few, kFew);
   };
   // the cut in bin l.bin
-  auto cut_in = [&](const Level l, bool by_mass, unsigned long long target) {
+  auto cut_in = [&](const Level coarse, bool by_mass, unsigned long long target) {
     const Cut old = cut;
+    Level l = coarse;
+    bool fine = false;
+    auto part_of = [&](float x) { return 255u - (uint32_t)min(255, max(0, (int)(((top - x) * scale - (float)(255u - coarse.bin)) * 256.f))); };
     auto member = [&](uint32_t key, uint32_t id) {
-      return (key > old.key || (key == old.key && id <= old.id)) && bin_of(logit_of(key)) == l.bin;
+      const float x = logit_of(key);
+      return (key > old.key || (key == old.key && id <= old.id)) && bin_of(x) == coarse.bin && (!fine || part_of(x) == l.bin);
     };
+    if (listed && l.at.count > (uint32_t)kFew) {       // 256 parts of the bin
+      const Bins b = count_bins(sm, 1, coarse.above, [&](auto) {
+        each([&](bool on, uint32_t key, uint32_t id, auto weigh) { hist_add_one(sm, on && member(key, id), part_of(logit_of(key)), weigh()); });
+      });
+      l = crossing(sm, b, by_mass, target);
+      fine = true;
+    }
     if (listed && l.at.count <= (uint32_t)kFew) {
       const int few = gather_few(member);
       if (t < few) {
-        const uint32_t key = sm.few_key[t], id = sm.few_id[t], w = sm.few_w[t];
+        const uint4 me = sm.few[t];
+        const uint32_t key = me.x, id = me.y, w = me.z;
         Tally b = l.above;
-#pragma unroll 4
+#pragma unroll 8
         for (int j = 0; j < few; ++j) {
-          const uint32_t k = sm.few_key[j];
-          if (k > key || (k == key && sm.few_id[j] < id)) b.mass += sm.few_w[j], ++b.count;
+          const uint4 o = sm.few[j];
+          const bool first = (o.x > key) | ((o.x == key) & (o.y < id));
+          b.mass += first ? o.z : 0u, b.count += first;
         }
         const unsigned long long x = by_mass ? b.mass : b.count;
         if (x < target && target - x <= (by_mass ? w : 1u)) sm.cut = {key, id, {b.mass + w, b.count + 1u}};
@@ -460,29 +635,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   auto need_of = [&](unsigned long long mass) { return min(max(1ull, (unsigned long long)ceil((double)top_p * (double)mass)), mass); };
 
   bool p_done = false;
-  if (has_k && top_k <= n * kWarps) {
+  if (has_k && top_k <= n * kGroups) {
     // a rounded quotient can put an id of weight below the point where none should have any: 1e-6 of the logits covers it
     const float near = fmaxf(least, top - 22.f * temp - fabsf(top) * 1e-6f);
-    gather([&](float x) { return x >= near; });
-    cut.in.count = *(n > 1 ? cl.map_shared_rank(&sm.n_list, 0) : &sm.n_list);
-    listed = cut.in.count <= (uint32_t)kList;
-    meet();                                            // (read by all)
+    listed = gather([&](float x) { return x >= near; }) <= (uint32_t)kList;
     if (listed) {
       if (rank > 0) return;
       const float span = top - near;
       scale = span > 0.f ? 255.f / span : 0.f;
-      const Bins b = key_bins();
+      Tally rest;
+      const Bins b = key_bins(-INFINITY, rest);
       cut.in = bins_sum(sm, b);
       if ((uint32_t)top_k < cut.in.count) cut_in(crossing(sm, b, false, top_k), false, top_k);
-    } else if (rank == 0 && t == 0) {
-      sm.n_list = 0u;
     }
   }
   if ((has_k || has_p) && !listed) {
-    const Bins b = key_bins();
-    cut.in = bins_sum(sm, b);
-    has_k = has_k && (uint32_t)top_k < cut.in.count;
-    unsigned long long target = has_k ? (unsigned long long)top_k : need_of(cut.in.mass);
+    // (most ids are far from the maximum, and few cuts: they are left out of the histogram first)
+    Tally rest, sums;
+    Bins b;
+    unsigned long long target = 0ull;
+    bool some = false;
+    for (const float far : {kNear, 22.f}) {
+      scale = 255.f / (far * temp);
+      b = key_bins(far < 22.f ? top - far * temp : -INFINITY, rest);
+      sums = bins_sum(sm, b);
+      cut.in = {sums.mass + rest.mass, sums.count + rest.count};
+      some = has_k && (uint32_t)top_k < cut.in.count;
+      target = some ? (unsigned long long)top_k : has_p ? need_of(cut.in.mass) : 0ull;
+      if (target <= (some ? sums.count : sums.mass)) break;
+    }
+    has_k = some;
     // (a bin's ids to the list, or all down to it: the first CTA alone finds the cut and, in the first case, tells the others)
     auto find = [&](const Level l, bool by_mass) {
       const bool all = l.above.count + l.at.count <= (uint32_t)kList;
@@ -500,7 +682,6 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
       }
       if (all) return;
       if (rank == 0) {
-        if (t == 0) sm.n_list = 0u;
         if (t < n) *(n > 1 ? cl.map_shared_rank(&sm.cut, t) : &sm.cut) = cut;
       }
       meet();
@@ -527,13 +708,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     int i = warp;
     each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
       Tally y{0ull, 0u};
+      uint32_t w[8];
+      weight.eight(v, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (e >= left || !before_cut(key_of(v[e]), (uint32_t)(id + e))) continue;
-        const uint32_t w = weight(v[e]);
-        if (w >= w_min) y.mass += w, ++y.count;
+        const bool on = e < left && w[e] >= w_min && before_cut(key_of(v[e]), (uint32_t)(id + e));
+        y.mass += on ? w[e] : 0u, y.count += on;
       }
-      y.mass = warp_sum(y.mass);
+      y.mass = warp_sum36(y.mass);                     // (eight of 2^31 at most)
       if (lane == 0) sm.block[i] = y.mass, x.mass += y.mass;
       x.count += y.count;
       i += kWarps;
@@ -597,7 +779,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   // from the list (the first CTA alone)
   if (has_p && !p_done && cut.in.count > (uint32_t)kFew) {
     const unsigned long long need = need_of(cut.in.mass);
-    const Bins b = key_bins();
+    Tally rest;
+    const Bins b = key_bins(-INFINITY, rest);
     cut_in(crossing(sm, b, true, need), true, need);
     p_done = true;
   }
@@ -606,26 +789,29 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     const unsigned long long need = has_p && !p_done ? need_of(cut.in.mass) : ~0ull;
     uint32_t key = 0u, id = 0u, w = 0u;
     if (t < few) {
-      key = sm.few_key[t], id = sm.few_id[t], w = sm.few_w[t];
+      const uint4 me = sm.few[t];
+      key = me.x, id = me.y, w = me.z;
       unsigned long long b = 0ull;
       if (need != ~0ull) {
-#pragma unroll 4
+#pragma unroll 8
         for (int j = 0; j < few; ++j) {
-          const uint32_t k = sm.few_key[j];
-          if (k > key || (k == key && sm.few_id[j] < id)) b += sm.few_w[j];
+          const uint4 o = sm.few[j];
+          b += (o.x > key) | ((o.x == key) & (o.y < id)) ? o.z : 0u;
         }
       }
       if (b >= need || w < w_min) w = 0u;
     }
     __syncthreads();
-    if (t < few) sm.few_w[t] = w;
+    if (t < few) sm.few[t].z = w;
     const Tally in = block_sum(sm, {w, w > 0u});
     const unsigned long long drawn = min((unsigned long long)floor(u * (double)in.mass), in.mass - 1);
     if (w > 0u) {
       unsigned long long b = 0ull;
-#pragma unroll 4
-      for (int j = 0; j < few; ++j)
-        if (sm.few_id[j] < id) b += sm.few_w[j];
+#pragma unroll 8
+      for (int j = 0; j < few; ++j) {
+        const uint4 o = sm.few[j];
+        b += o.y < id ? o.z : 0u;
+      }
       if (b <= drawn && drawn < b + w) give(id, w, in);
     }
     return;
