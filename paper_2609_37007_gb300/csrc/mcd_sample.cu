@@ -63,7 +63,7 @@ struct Tally {
 // What a CTA tells the others.
 struct Told {
   float top, least;                    // its maximum, the least of its groups' maxima
-  int bad;
+  int bad, odd;                        // logits that do not fit; that are not quotients' plain operands
   uint32_t lo, hi;
   Tally sum;
 };
@@ -137,8 +137,8 @@ __device__ __forceinline__ void hist_add(Shared& sm, bool on, uint32_t bin, uint
 // W of a logit: its quotient with T, the exponential of the difference from the maximum's, in the steps that define them.  Eight of
 // a thread at a time, two an instruction, without branches.  The quotient is Markstein's (IBM J. Res. Dev. 34, 1990): from the
 // correctly rounded 1 / T two corrections by the exact remainder give the correctly rounded quotient while nothing under- or
-// overflows; elsewhere (`plain` false, or a logit far from 1) it is divided.  Rounding to a whole number is by adding 1.5 * 2^23, whose
-// last bits then are that number.
+// overflows; in other rows (`plain` false) it is divided.  Rounding to a whole number is by adding 1.5 * 2^23, whose last bits then
+// are that number.
 struct Weigh {
   float temp, inverse, z_top;
   bool plain;
@@ -149,14 +149,12 @@ struct Weigh {
     using namespace paged;
     auto both = [](float x) { return pack2(x, x); };
     uint64_t z[4];
-    bool near = plain;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) near &= ((__float_as_uint(v[e]) & 0x7fffffffu) - 0x27000000u) < 0x30000000u;      // 2^-49 .. 2^47
-    if (__all_sync(__activemask(), near)) {
+    if (plain) {
       const uint64_t inv = both(inverse), minus = both(-temp);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint64_t x = pack2(v[2 * e], v[2 * e + 1]), q0 = mul2(x, inv), q1 = fma2(fma2(q0, minus, x), inv, q0);
+        // (-1e30 for -inf: W is 0 all the same)
+        const uint64_t x = pack2(fmaxf(v[2 * e], -1e30f), fmaxf(v[2 * e + 1], -1e30f)), q0 = mul2(x, inv), q1 = fma2(fma2(q0, minus, x), inv, q0);
         z[e] = fma2(fma2(q1, minus, x), inv, q1);
       }
     } else {
@@ -194,8 +192,8 @@ struct Weigh {
       unpack2(s, p[0], p[1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {                    // (times 2^(n + 31): powers of two)
-        const uint32_t u = __float2uint_rd(__fmul_rn(p[i], __uint_as_float((__float_as_uint(y[i]) << 23) + (158u << 23))));
-        w[2 * e + i] = d[i] < -87.f ? 0u : u;
+        // (from -87 down: 0, as the definition has it)
+        w[2 * e + i] = __float2uint_rd(__fmul_rn(p[i], __uint_as_float((__float_as_uint(y[i]) << 23) + (158u << 23))));
       }
     }
   }
@@ -223,11 +221,15 @@ __device__ __forceinline__ Bins count_bins(Shared& sm, int n, Tally above, Each 
   else __syncthreads();
   Bins b{{0ull, 0u}, above};
   if (t < 256) {
-    for (int z = 0; z < n; ++z) {
-      const uint32_t* h = n > 1 ? cl.map_shared_rank(&sm.hist[0][0], z) : &sm.hist[0][0];
-      b.own.count += h[255 - t];
-      b.own.mass += h[511 - t] + ((unsigned long long)h[767 - t] << 16);
+    uint32_t x[kMaxCluster][3];                        // (all on their way together: a turn each, they took 8,000 cycles)
+#pragma unroll
+    for (int z = 0; z < kMaxCluster; ++z) {
+      const uint32_t* h = n > 1 ? cl.map_shared_rank(&sm.hist[0][0], min(z, n - 1)) : &sm.hist[0][0];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) x[z][i] = z < n ? h[256 * i + 255 - t] : 0u;
     }
+#pragma unroll
+    for (int z = 0; z < kMaxCluster; ++z) b.own.count += x[z][0], b.own.mass += x[z][1] + ((unsigned long long)x[z][2] << 16);
     Tally run = b.own;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -351,19 +353,22 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   Told mine = {};
   {
     float most = -INFINITY;
-    bool bad = false;
+    bool bad = false, odd = false;
     each_eight(row, lo, hi, [&](int, int left, const float (&v)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (e >= left) continue;
         most = fmaxf(most, v[e]);
         bad |= !(v[e] <= 3.40282347e38f);              // NaN or +inf
+        const uint32_t size = __float_as_uint(v[e]) & 0x7fffffffu;      // 2^-99 .. 2^95, 0 or -inf
+        odd |= size - 0x0e000000u >= 0x61000000u && size != 0u && size != 0x7f800000u;
       }
     });
 #pragma unroll
     for (int w = 8; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
     if ((lane & 15) == 0) sm.fred[t >> 4] = most;
     mine.bad = __syncthreads_or(bad);
+    mine.odd = __syncthreads_or(odd);
     mine.top = -INFINITY, mine.least = INFINITY;
     for (int i = 0; i < kGroups; ++i) mine.top = fmaxf(mine.top, sm.fred[i]), mine.least = fminf(mine.least, sm.fred[i]);
   }
@@ -375,8 +380,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   if (n > 1) cl.barrier_wait();                        // (the others have started)
   tell(0);
   float top = -INFINITY, least = INFINITY;
+  bool plain = temp > 1e-6f && temp < 1e6f;
   bool bad = !(temp >= 0.f && temp <= 3.40282347e38f) || isnan(top_p) || isnan(min_p) || !(u >= 0. && u < 1.);
-  for (int z = 0; z < n; ++z) top = fmaxf(top, sm.told[0][z].top), least = fminf(least, sm.told[0][z].least), bad |= sm.told[0][z].bad != 0;
+  for (int z = 0; z < n; ++z) top = fmaxf(top, sm.told[0][z].top), least = fminf(least, sm.told[0][z].least), bad |= sm.told[0][z].bad != 0, plain &= sm.told[0][z].odd == 0;
   bad |= top == -INFINITY;
   auto give = [&](uint32_t id, unsigned long long w, Tally in) {
     a.ids[r] = (int)id;
@@ -396,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   bool has_k = top_k > 0 && top_k < V;
   const bool greedy = temp == 0.f || !(fabsf(z_top) <= 3.40282347e38f) || top_k == 1 || top_p <= 0.f;
   const uint32_t w_min = min_p > 0.f ? max(1u, (uint32_t)ceil((double)fminf(min_p, 1.f) * 2147483648.)) : 1u;
-  const Weigh weight{temp, __fdiv_rn(1.f, temp), z_top, temp > 1e-15f && temp < 1e15f};
+  const Weigh weight{temp, __fdiv_rn(1.f, temp), z_top, plain && fabsf(top) < 1e28f};
 
   bool listed = false;
   // f(on, key, id, weigh) for the CTA's share of the row, or (the first CTA alone) of the list, warp by warp
@@ -524,16 +530,17 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   auto from_id = [V](uint32_t id) { return (uint32_t)(V - 1) - id; };
 
   // ---- cuts
-  Cut cut{0u, 0xffffffffu, {0ull, 0u}};
+  Cut cut{0x007fffffu, 0xffffffffu, {0ull, 0u}};       // (the key of -inf: nothing is cut)
+  auto logit_before_cut = [&](float x, uint32_t id) {
+    const float c = logit_of(cut.key);
+    return x > c || (x == c && id <= cut.id);
+  };
   auto before_cut = [&](uint32_t key, uint32_t id) { return key > cut.key || (key == cut.key && id <= cut.id); };
-  // steps of the histograms: from the maximum down to kNear T below it, to 22 T where W is 0 (2^31 e^-21.5 < 1), or to the list's end
-  constexpr float kNear = 8.f;
+  // steps of the histograms: from the maximum down to where W is 0 (2^31 e^-21.5 < 1), or to the list's end
   float scale = 255.f / (22.f * temp);
   auto bin_of = [&](float x) { return 255u - (uint32_t)min(255, (int)((top - x) * scale)); };
-  // (ids below `low` are counted in the last bin's place: `rest` is their sum)
-  auto key_bins = [&](float low, Tally& rest) {
-    Tally out{0ull, 0u};
-    const Bins b = count_bins(sm, listed ? 1 : n, {0ull, 0u}, [&](auto) {
+  auto key_bins = [&] {
+    return count_bins(sm, listed ? 1 : n, {0ull, 0u}, [&](auto) {
       if (listed) {
         each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
           hist_add_one(sm, on && before_cut(key, id), bin_of(logit_of(key)), weigh());
@@ -543,26 +550,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
           uint32_t w[8];
           weight.eight(v, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool on = e < left && w[e] > 0u, far = on && v[e] < low;
-            out.mass += far ? w[e] : 0u, out.count += far;
-            hist_add_one(sm, on && !far, bin_of(v[e]), w[e]);
-          }
+          for (int e = 0; e < 8; ++e) hist_add_one(sm, e < left && w[e] > 0u, bin_of(v[e]), w[e]);
         });
       }
     });
-    rest = out;
-    if (!listed) {
-      rest = block_sum(sm, out);
-      if (n > 1) {
-        mine.sum = rest;
-        tell(1);
-        rest = {0ull, 0u};
-        for (int z = 0; z < n; ++z) rest.mass += sm.told[1][z].sum.mass, rest.count += sm.told[1][z].sum.count;
-        meet();
-      }
-    }
-    return b;
   };
   // the few ids that `want` takes, to the short list
   auto gather_few = [&](auto want) {
@@ -643,28 +634,16 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
       if (rank > 0) return;
       const float span = top - near;
       scale = span > 0.f ? 255.f / span : 0.f;
-      Tally rest;
-      const Bins b = key_bins(-INFINITY, rest);
+      const Bins b = key_bins();
       cut.in = bins_sum(sm, b);
       if ((uint32_t)top_k < cut.in.count) cut_in(crossing(sm, b, false, top_k), false, top_k);
     }
   }
   if ((has_k || has_p) && !listed) {
-    // (most ids are far from the maximum, and few cuts: they are left out of the histogram first)
-    Tally rest, sums;
-    Bins b;
-    unsigned long long target = 0ull;
-    bool some = false;
-    for (const float far : {kNear, 22.f}) {
-      scale = 255.f / (far * temp);
-      b = key_bins(far < 22.f ? top - far * temp : -INFINITY, rest);
-      sums = bins_sum(sm, b);
-      cut.in = {sums.mass + rest.mass, sums.count + rest.count};
-      some = has_k && (uint32_t)top_k < cut.in.count;
-      target = some ? (unsigned long long)top_k : has_p ? need_of(cut.in.mass) : 0ull;
-      if (target <= (some ? sums.count : sums.mass)) break;
-    }
-    has_k = some;
+    const Bins b = key_bins();
+    cut.in = bins_sum(sm, b);
+    has_k = has_k && (uint32_t)top_k < cut.in.count;
+    unsigned long long target = has_k ? (unsigned long long)top_k : need_of(cut.in.mass);
     // (a bin's ids to the list, or all down to it: the first CTA alone finds the cut and, in the first case, tells the others)
     auto find = [&](const Level l, bool by_mass) {
       const bool all = l.above.count + l.at.count <= (uint32_t)kList;
@@ -712,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
       weight.eight(v, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool on = e < left && w[e] >= w_min && before_cut(key_of(v[e]), (uint32_t)(id + e));
+        const bool on = e < left && w[e] >= w_min && logit_before_cut(v[e], (uint32_t)(id + e));
         y.mass += on ? w[e] : 0u, y.count += on;
       }
       y.mass = warp_sum36(y.mass);                     // (eight of 2^31 at most)
@@ -779,8 +758,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   // from the list (the first CTA alone)
   if (has_p && !p_done && cut.in.count > (uint32_t)kFew) {
     const unsigned long long need = need_of(cut.in.mass);
-    Tally rest;
-    const Bins b = key_bins(-INFINITY, rest);
+    const Bins b = key_bins();
     cut_in(crossing(sm, b, true, need), true, need);
     p_done = true;
   }
