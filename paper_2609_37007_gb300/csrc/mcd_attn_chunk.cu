@@ -119,6 +119,13 @@ __device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, i
   return __funnelshift_r(__ldg(row + w), next, j0 & 31) & in;
 }
 
+// Pairs of bf16: the larger of m's and the sizes of w's, NaN where either is.
+__device__ __forceinline__ uint32_t largest_size(uint32_t m, uint32_t w) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(w & 0x7fff7fffu));
+  return d;
+}
+
 // Packed vector r of the pair over the keys of `keys`, key by key, by a warp; lane d holds dimensions d * D / 32 ...
 template <int D, bool kWin>
 __device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, const Pack& pack, int r, Span keys, Gap gap, float& m,
@@ -286,12 +293,12 @@ __global__ void __launch_bounds__(kCThreads, 1)
   // Tiles whose V warp 10 looks at, from this one on: those that end behind the keys or hold a key that some row does
   // not see.  Number n of these has barriers n % (S / 2) of its own (no more V tiles are in the ring): warp 10 waits
   // for every phase of them, as it could not for the ring's, whose earlier phases it has no part in.
-  // With a window also the first ones, up to the last window's start: `early` of them, in whole rounds of the ring (or all),
-  // so that the ring's barriers are the same number of phases, `late`, behind the rounds in every V stage.
+  // With a window also the first ones, up to the last window's start: `early` of them.  The ring's barrier of a V stage is as
+  // many phases behind the rounds (late_at: odd or even) as the stage has early tiles.
   const int seen_by_all = max(0, (min(keys.hi, q.cached + (a.mask ? 0 : i_first + 1) - gap.gap) - keys.lo) / kCTile);
   int early = 0;
-  if (kWin) early = min(n_tiles, (max(0, (lows.to - gap.gap - keys.lo + kCTile - 1) / kCTile) + S / 2 - 1) / (S / 2) * (S / 2));
-  const uint32_t late = kWin ? early / (S / 2) & 1 : 0;
+  if (kWin) early = min(n_tiles, max(0, (lows.to - gap.gap - keys.lo + kCTile - 1) / kCTile));
+  auto late_at = [&](uint32_t j) { return kWin ? (early + S / 2 - 1 - j % (S / 2)) / (S / 2) & 1u : 0u; };
   const int first_look = max(seen_by_all, early);
 
   const uint32_t tmem = *tmem_slot;
@@ -301,7 +308,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
   auto look_tile = [&](int j) { return j >= first_look ? j - first_look + early : j < early ? j : -1; };
   auto look = [&](uint32_t i) { return i & 1 ? look_tile((int)(i >> 1)) : -1; };
   auto load_bar = [&](uint32_t i) { return look(i) < 0 ? &full[i % S] : &v_full[look(i) % (S / 2)]; };
-  auto load_phase = [&](uint32_t i) { return look(i) < 0 ? (i / S & 1) ^ (late & i) : (uint32_t)look(i) / (S / 2) & 1; };
+  auto load_phase = [&](uint32_t i) { return look(i) < 0 ? (i / S & 1) ^ (i & 1 ? late_at(i >> 1) : 0u) : (uint32_t)look(i) / (S / 2) & 1; };
   auto stage = [&](uint32_t i) { return smem + L::kRing + i % S * L::kTileBytes; };
 
   float m = -INFINITY, l = 0.f;                        // softmax threads: of their row
@@ -396,7 +403,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
         const uint32_t at_k = at_v + 1 < S ? at_v + 1 : 0;
         if (j + 1 < n_tiles && !wait(&full[at_k], at_k ? phase : phase ^ 1)) break;
         if (const int n = look_tile(j); n < 0) {
-          if (!wait(&full[at_v], phase ^ late)) break;
+          if (!wait(&full[at_v], phase ^ late_at(j))) break;
         } else if (!wait(&v_full[n % (S / 2)], n / (S / 2) & 1) || !wait(&v_seen[n % (S / 2)], n / (S / 2) & 1)) {
           break;
         }
@@ -419,17 +426,43 @@ __global__ void __launch_bounds__(kCThreads, 1)
       if (!warp_wait(load_bar(i), load_phase(i), a.err, abort_flag)) break;
       uint8_t* v = stage(i);
       const int from = keys.lo + j * kCTile, k0 = kWin ? gap.at(from) : from;
-      const int first = j < early ? 0 : max(0, q.cached - k0), end = min(kCTile, keys.hi - from);
-      bool bad = false;
-#pragma unroll 4
-      for (int n = first * 8 + lane; n < end * 8; n += 32)
-        for (int c = 0; c < kDC; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(v + c * kChunk + n * 16);
-          bad |= !(bf16x2_finite(x.x) && bf16x2_finite(x.y) && bf16x2_finite(x.z) && bf16x2_finite(x.w));
+      const int end = min(kCTile, keys.hi - from);
+      // keys lo .. hi of the tile become zeros
+      auto clear_keys = [&](int lo, int hi) {
+        for (int n = lo * 8 + lane; n < hi * 8; n += 32)
+          for (int c = 0; c < kDC; ++c) *reinterpret_cast<uint4*>(v + c * kChunk + n * 16) = make_uint4(0u, 0u, 0u, 0u);
+      };
+      // (the largest size of all, several pieces on their way at a time: each looked at as it came, a tile took 8,200 cycles)
+      uint32_t most[4] = {0u, 0u, 0u, 0u};
+      auto look_at = [&](int lo, int hi) {
+        constexpr int kAhead = 8 / kDC;
+        for (int n = lo * 8 + lane; n < hi * 8; n += 32 * kAhead) {
+          uint4 x[kAhead][kDC];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int c = 0; c < kDC; ++c)
+              x[i][c] = n + 32 * i < hi * 8 ? *reinterpret_cast<const uint4*>(v + c * kChunk + (n + 32 * i) * 16) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int c = 0; c < kDC; ++c) {
+              most[0] = largest_size(most[0], x[i][c].x), most[1] = largest_size(most[1], x[i][c].y);
+              most[2] = largest_size(most[2], x[i][c].z), most[3] = largest_size(most[3], x[i][c].w);
+            }
         }
-      if (bad) *odd = 1;
-      for (int n = end * 8 + lane; n < kCTile * 8; n += 32)
-        for (int c = 0; c < kDC; ++c) *reinterpret_cast<uint4*>(v + c * kChunk + n * 16) = make_uint4(0u, 0u, 0u, 0u);
+      };
+      const int chunk = max(0, q.cached - k0);         // the first new row
+      if (j < early) {                                 // in front of every window: zeros; in front of some: looked at
+        const int sinks = min(max(a.sinks - k0, 0), end), none = min(max(lows.from - k0, sinks), end), all = min(max(lows.to - k0, none), end);
+        clear_keys(sinks, none);
+        look_at(none, all);
+        look_at(max(all, min(chunk, end)), end);
+      } else {
+        look_at(chunk, end);
+      }
+      if (!(bf16x2_finite(most[0]) && bf16x2_finite(most[1]) && bf16x2_finite(most[2]) && bf16x2_finite(most[3]))) *odd = 1;
+      clear_keys(end, kCTile);
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) mbar_arrive(&v_seen[look_tile(j) % (S / 2)]);
@@ -462,7 +495,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
     const bool live = base < n_vecs;
     // keys below this position are seen by every row of the warp
     const int clear = q.cached + (a.mask ? 0 : pack.row(base) + 1);
-    const int low = kWin ? window_low(a, q, row) : 0, low_warp = window_lows<kWin>(a, q, 0, pack.row(min(base + 32, n_vecs) - 1)).to;
+    const int low = kWin ? window_low(a, q, row) : 0;
     float mc = 0.f;                                    // c * (the maximum in use)
     bool ok = true;
     for (int j = 0; j < n_mine; ++j) {
@@ -481,7 +514,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_loaded(x[c]);
         const int from = keys.lo + j * kCTile, k0 = kWin ? gap.at(from) : from;
-        if (k0 + kCTile > clear || from + kCTile > keys.hi || !in_window<kWin>(a, low_warp, k0, kCTile)) {
+        if (kWin ? look_tile(j) >= 0 : k0 + kCTile > min(clear, keys.hi)) {      // (with a window: hidden from some row of the pair)
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int pos = k0 + 32 * c, left = keys.hi - from - 32 * c;
