@@ -392,12 +392,18 @@ __global__ void __launch_bounds__(kSThreads, 3)
     bool odd = false;
     if (edge && __any_sync(0xffffffffu, hidden)) {
       const int first = cut ? 0 : max(q.cached - key0, 0), n = (min(left, 16) - first) * 8;
-      for (int i = lane; i < n; i += 32)
+      uint32_t most = 0u;                              // (all pieces on their way together)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
         for (int c = 0; c < kDC; ++c) {
-          const uint4 v = *reinterpret_cast<const uint4*>(v_tile + c * kChunk + (16 * warp + first) * 128 + i * 16);
-          odd |= !(bf16x2_finite(v.x) && bf16x2_finite(v.y) && bf16x2_finite(v.z) && bf16x2_finite(v.w));
+          const int i = lane + 32 * k;
+          const uint4 v = i < n ? *reinterpret_cast<const uint4*>(v_tile + c * kChunk + (16 * warp + first) * 128 + i * 16)
+                                : make_uint4(0u, 0u, 0u, 0u);
+          most = largest_size(largest_size(most, v.x), v.y);
+          most = largest_size(largest_size(most, v.z), v.w);
         }
-      odd = __any_sync(0xffffffffu, odd);
+      odd = __any_sync(0xffffffffu, !bf16x2_finite(most));
     }
     if (!odd) {
       const uint4 ph = make_uint4(hi[0], hi[1], hi[2], hi[3]), pl = make_uint4(lo[0], lo[1], lo[2], lo[3]);

@@ -290,6 +290,13 @@ __device__ __forceinline__ bool bf16x2_finite(uint32_t w) {
   return (w & 0x7F80u) != 0x7F80u && (w & 0x7F800000u) != 0x7F800000u;
 }
 
+// Pairs of bf16: the larger of m's and the sizes of w's, NaN where either is.
+__device__ __forceinline__ uint32_t largest_size(uint32_t m, uint32_t w) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(w & 0x7fff7fffu));
+  return d;
+}
+
 // Launch with clusters of `cluster` CTAs along x.
 template <class K, class... Args>
 cudaError_t launch_clusters(K* kernel, dim3 grid, int threads, int cluster, size_t smem, cudaStream_t st, const Args&... args) {

@@ -119,13 +119,6 @@ __device__ __forceinline__ uint32_t seen_word(const AttnArgs& a, const Seq& q, i
   return __funnelshift_r(__ldg(row + w), next, j0 & 31) & in;
 }
 
-// Pairs of bf16: the larger of m's and the sizes of w's, NaN where either is.
-__device__ __forceinline__ uint32_t largest_size(uint32_t m, uint32_t w) {
-  uint32_t d;
-  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(w & 0x7fff7fffu));
-  return d;
-}
-
 // Packed vector r of the pair over the keys of `keys`, key by key, by a warp; lane d holds dimensions d * D / 32 ...
 template <int D, bool kWin>
 __device__ __noinline__ void slow_row(const AttnArgs& a, const Seq& q, int s, int h, const Pack& pack, int r, Span keys, Gap gap, float& m,
