@@ -56,6 +56,14 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
 
+// The cluster's barrier, for threads whose warp may not be together at it, and ordered with the memory accesses around it.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  cluster_arrive();
+  cluster_wait();
+}
+
 struct Tally {
   unsigned long long mass;
   uint32_t count;
@@ -217,7 +225,7 @@ __device__ __forceinline__ Bins count_bins(Shared& sm, int n, Tally above, Each 
   for (int i = t; i < 3 * 256; i += kThreads) (&sm.hist[0][0])[i] = 0u;
   __syncthreads();
   each([&](bool on, uint32_t bin, uint32_t w) { hist_add(sm, on, bin, w); });
-  if (n > 1) cl.sync();
+  if (n > 1) cluster_sync();
   else __syncthreads();
   Bins b{{0ull, 0u}, above};
   if (t < 256) {
@@ -240,7 +248,7 @@ __device__ __forceinline__ Bins count_bins(Shared& sm, int n, Tally above, Each 
     if (lane == 31) sm.red[t >> 5] = run;
     b.before.mass += run.mass - b.own.mass, b.before.count += run.count - b.own.count;
   }
-  if (n > 1) cl.sync();                                // (nobody clears what another still reads)
+  if (n > 1) cluster_sync();                                // (nobody clears what another still reads)
   else __syncthreads();
   for (int i = 0; i < (t >> 5) && t < 256; ++i) b.before.mass += sm.red[i].mass, b.before.count += sm.red[i].count;
   return b;
@@ -338,10 +346,10 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   const int V = a.vocab, per = ((V + n - 1) / n + 7) / 8 * 8, lo = min(V, rank * per), hi = min(V, lo + per);
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
   auto meet = [&] {
-    if (n > 1) cl.sync();
+    if (n > 1) cluster_sync();
     else __syncthreads();
   };
-  if (n > 1) cl.barrier_arrive();
+  if (n > 1) cluster_arrive();
   tc::pdl_wait();
   tc::pdl_trigger();
   const float temp = a.temperature ? __ldg(a.temperature + r) : 1.f, top_p = a.top_p ? __ldg(a.top_p + r) : 1.f,
@@ -377,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
     if (t < n) *(n > 1 ? cl.map_shared_rank(&sm.told[what][rank], t) : &sm.told[what][0]) = mine;
     meet();
   };
-  if (n > 1) cl.barrier_wait();                        // (the others have started)
+  if (n > 1) cluster_wait();                        // (the others have started)
   tell(0);
   float top = -INFINITY, least = INFINITY;
   bool plain = temp > 1e-6f && temp < 1e6f;
@@ -500,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
       }
       if (t == 0) sm.n_list = sum;
     }
-    cl.sync();                                         // (the lists have been read)
+    cluster_sync();                                         // (the lists have been read)
     return sum;
   };
   // narrows [at.x, at.y], a range of what `of` gives, to the one value where the running sum over descending values reaches the
