@@ -2,7 +2,8 @@
 // KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
 //
 // Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 50.7 us, 5.2 TB/s (fp32: 205 us, 2.6 TB/s);
-// 4 x 2 to 4 rows over up to 120,000: 247 us, 6.2 TB/s of 6.8 measured for a copy.  fp32 chunks: 68.6 us for 24 sequences of 1
+// 4 x 2 to 4 rows over up to 120,000: 245 us, 6.2 TB/s of 6.8 measured for a copy; 128 single rows with windows of 4,096 keys and 4
+// sinks over up to 60,000: 344 us, 6.0 TB/s; one with a window of 1,024: 8.5 us.  fp32 chunks: 68.6 us for 24 sequences of 1
 // to 200 rows over up to 600 (4 heads of 64), a sixth of the fp32 rate: tiles of 64 rows and 64 keys are half empty, and 16
 // warps an SM (their registers) issue every other cycle (packed products, half the instructions: the same time).
 #include <algorithm>
@@ -630,13 +631,15 @@ AttnArgs planned(const mcd_paged_kv& kv, const mcd_chunks& ch, int group, int wi
   return a;
 }
 
+int64_t workspace_bytes_of(const AttnArgs& a) {
+  if (a.kv.dtype != MCD_WEIGHT_BF16 || !route_of(a.ch, a.group).steps) return 0;
+  const StepPlan p = plan_step(a);
+  return p.in_workspace ? 4ll * a.kv.n_kv_heads * a.ch.n_seqs * p.splits * kSVecs * (a.kv.head_dim + 4) : 0;
+}
 // (a window of 0: none)
 int64_t workspace_bytes_of(const mcd_paged_kv* kv, const mcd_chunks* chunks, int32_t n_q_heads, int32_t window, int32_t sinks) {
   if (check_kv(kv) != MCD_OK || check_chunks(chunks, kv) != MCD_OK || no_rows(chunks) || n_q_heads <= 0) return 0;
-  const AttnArgs a = planned(*kv, *chunks, std::max(1, n_q_heads / kv->n_kv_heads), window, sinks);
-  if (kv->dtype != MCD_WEIGHT_BF16 || !route_of(a.ch, a.group).steps) return 0;
-  const StepPlan p = plan_step(a);
-  return p.in_workspace ? 4ll * kv->n_kv_heads * chunks->n_seqs * p.splits * kSVecs * (kv->head_dim + 4) : 0;
+  return workspace_bytes_of(planned(*kv, *chunks, std::max(1, n_q_heads / kv->n_kv_heads), window, sinks));
 }
 
 mcd_status attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* chunks, int32_t n_q_heads, const void* q,
@@ -656,9 +659,9 @@ mcd_status attention(const mcd_paged_kv* kv, int32_t layer, const mcd_chunks* ch
   if (q_stride < width || out_stride < width) return MCD_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || q_stride * esize(kv->dtype) % 16 || out_stride * esize(kv->dtype) % 16)
     return MCD_ERR_UNSUPPORTED;
-  const int64_t need = workspace_bytes_of(kv, chunks, n_q_heads, window, sinks);
-  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
   AttnArgs a = planned(*kv, *chunks, n_q_heads / kv->n_kv_heads, window, sinks);
+  const int64_t need = workspace_bytes_of(a);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return MCD_ERR_INVALID_ARG;
   a.q = q, a.out = out, a.mask = mask, a.err = err;
   a.q_stride = q_stride, a.out_stride = out_stride;
   a.layer = layer, a.mask_words = mask_words;

@@ -17,10 +17,12 @@
 // S to P takes a tile's softmax about 1,700 cycles (exponentials, packing and tensor memory) and its products
 // about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
 // the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
-// up to 8,500 keys (370 to 382 us; 0.66 of what a library product reaches; tensor pipe 55 % active).
+// up to 8,500 keys (361 us; 0.69 of what a library product reaches; tensor pipe 55 % active).  With a window, 17,004 rows over
+// 2,048 keys and 4 sinks each: 333 us, 0.89 PFLOP/s; 18 key tiles a CTA, of which the sinks' and four at the window's ends are seen in
+// part, and 3 of them take 15 us where all else takes 1.4 us a tile.
 // A CTA fills an SM, and takes about 8 us to start and end (1.5 to its place in the lists, 3 to 4 to the first scores, 2 to
 // their P, 1 to 2 to the rows of o written and the next CTA): the pairs with most keys start first (32 x 65 rows over 200 to
-// 1,500 keys: 45.4 us, in the sequences' own order 59).
+// 1,500 keys: 43.9 us, in the sequences' own order 59).
 // P is rounded to one bf16, off by 2^-8 of a probability at most, and l sums it unrounded: a hi + lo pair, as the step
 // kernel multiplies, would double the second product, half of the tensor work.  Relative to the norm of the result the
 // error is 2.2e-3 for those trees and 2.3e-3 for the long prompts; the rounding of the result alone gives 1.7e-3.

@@ -4,6 +4,10 @@
 // 8 bits is max |v| / 448 = i max |r gain| / 448, so that q and the maximum are found in one pass and joined once; the row
 // stays in registers between its load and its store.
 // What bounds it: one read of x and the residual, one write of the sum and of y; for a few rows the chain load -> join -> store.
+// 30,011 rows of 4,096, bf16 in, sum and residual, 8 bits out: 154 us, 5.6 TB/s (0.84 of a copy; bf16 out 162, fp32 sums 228 us
+// or 7.0 TB/s).  A thread has 8 or 16 elements and a row as many threads as that takes, so that the SM's 2,048 threads have
+// 64 bytes each on their way: 4,096 elements on 512 threads 156, on 256 of two chunks 157, on 128 of four 173 us; 1,024 on a warp
+// of four chunks 89 against 72.  CTAs that stay and load the next row under the join took 296 (64 registers: half the threads).
 #include <cmath>
 
 #include "mcd_cache.cuh"

@@ -13,6 +13,11 @@
 //     as above; where they are too many, those of the crossing bin alone, and the draw is from the row;
 //   neither: the draw is from the row: sums of W of blocks of 256 ids, the block in which the target is crossed, the id.
 // Order never changes a result: whole numbers add up to the same sum.
+//
+// What bounds it: weights, about 30 operations each (the definition rounds every product and sum), barriers of the cluster (2,000
+// cycles each) and chains of small steps.  One row of 2,048, k = 50: 7 us on the GPU; of 131,072: 16 us, with top_p alone and 20,000
+// ids left 46.  128 rows of 2,048 with mixed settings 15.5 us, 96 of 131,072 (bf16) 70: the rows with large sets, a fifth, are
+// waited for.  Clusters: a CTA has 8,192 ids of a row, or an eighth of it.
 #include <cooperative_groups.h>
 
 #include <cmath>
