@@ -717,7 +717,7 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && keys / (2 * a.splits) >= 2 * kCTile)
     a.splits *= 2;
   // Order costs a CTA 25 ns a sequence, and what it saves is the last CTAs' time: worth it for few of either (65 rows over 200
-  // to 1,500 keys each: 32 sequences 45.4 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
+  // to 1,500 keys each: 32 sequences 43.9 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
   a.ranked = a.ch.n_seqs <= kRanked && a.ch.n_seqs * pairs * a.kv.n_kv_heads * a.splits <= 256ll * sm_count();
   // (ordered sequences leave no slots between them)
   const long long grid = (a.ranked ? pairs : slots) * a.kv.n_kv_heads * a.splits;
