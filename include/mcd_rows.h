@@ -39,7 +39,8 @@ enum { MCD_E4M3 = 3 };
  *   y_scale    dev float [n_rows] with MCD_E4M3, else not looked at
  * Strides are in elements, at least width; rows and gain are 16-byte aligned, width at most 16,384
  * (MCD_ERR_UNSUPPORTED otherwise).  sum may be residual, and sum or y may be x or residual, of the same type and
- * stride; apart from that an output overlaps neither an input nor the other outputs (MCD_ERR_INVALID_ARG).  No rows: MCD_OK. */
+ * stride; apart from that an output overlaps neither an input nor the other outputs (MCD_ERR_INVALID_ARG; rows of one stride
+ * may lie beside each other, of two strides what lies between each other's rows counts as overlapping).  No rows: MCD_OK. */
 mcd_status mcd_norm_rows(int32_t n_rows, int32_t width, const void* x, int64_t x_stride, int32_t x_dtype,
                          const void* residual, int64_t residual_stride, void* sum, int64_t sum_stride,
                          int32_t res_dtype, int32_t norm, const float* gain, float eps, void* y, int64_t y_stride,
@@ -66,7 +67,8 @@ mcd_status mcd_norm_rows(int32_t n_rows, int32_t width, const void* x, int64_t x
  *   kept         dev int32 [n_rows], optional: how many ids were left
  *   err          dev int32, zeroed by the caller: MCD_ERR_INVALID_ARG when a row has a NaN, +inf or nothing but -inf, or a
  *                setting that is NaN or out of its range; such a row has id -1, probability 0 and 0 ids left
- * Rows are 16-byte aligned, vocab is at most 262,144 (MCD_ERR_UNSUPPORTED otherwise).  Outputs overlap nothing. */
+ * Rows are 16-byte aligned, vocab is at most 262,144 (MCD_ERR_UNSUPPORTED otherwise).  Outputs and err overlap nothing
+ * (MCD_ERR_INVALID_ARG).  No rows: MCD_OK. */
 mcd_status mcd_sample_rows(int32_t n_rows, int32_t vocab, const void* logits, int64_t stride, int32_t dtype,
                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                            const double* u, int32_t* ids, float* probs, int32_t* kept, int32_t* err, void* stream);

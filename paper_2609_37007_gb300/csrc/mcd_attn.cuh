@@ -106,18 +106,19 @@ struct Gap {
 template <bool kWin>
 __device__ __forceinline__ Gap gap_of(const AttnArgs& a, int low, int tile) {
   if (!kWin) return {0, 0};
-  const int edge = (int)(((long long)a.sinks + tile - 1) / tile * tile), start = low / tile * tile;
-  return start > edge ? Gap{edge, start - edge} : Gap{0, 0};
+  const long long edge = ((long long)a.sinks + tile - 1) / tile * tile;
+  const int start = low / tile * tile;
+  return start > edge ? Gap{(int)edge, start - (int)edge} : Gap{0, 0};
 }
 // Whether some row whose window starts at `low` or later sees one of the n positions from pos on.
 template <bool kWin>
 __device__ __forceinline__ bool touched(const AttnArgs& a, int low, int pos, int n) {
-  return !kWin || pos + n > low || pos < a.sinks;
+  return !kWin || pos > low - n || pos < a.sinks;
 }
 // Whether a window that starts at `low` or before hides none of the n positions from pos on.
 template <bool kWin>
 __device__ __forceinline__ bool in_window(const AttnArgs& a, int low, int pos, int n) {
-  return !kWin || pos >= low || pos + n <= a.sinks;
+  return !kWin || pos >= low || pos <= a.sinks - n;
 }
 
 // Whether packed vectors of row i (of the sequence's new rows) see key `pos`; without a window keys below q.cached are seen by

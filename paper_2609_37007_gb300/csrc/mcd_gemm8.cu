@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
         if (z < g.splits) v.x += x[z].x, v.y += x[z].y, v.z += x[z].z, v.w += x[z].w;
       if (m0 + 4 * lane < g.M) store4_scaled<T>(g, n0 + c, m0 + 4 * lane, v);
     }
+    __syncwarp();
     cl.sync();                                         // nobody leaves while others read
   }
   tc_fence_before();
@@ -534,10 +535,12 @@ extern "C" mcd_status mcd_tc_gemm_e4m3(int32_t M, int32_t N, int32_t K, const vo
   if (M == 0 || N == 0) return MCD_OK;
   if (!A || !B || !Y || K == 0 || lda < K || ldb < K || ldy < M) return MCD_ERR_INVALID_ARG;
   // (65,535 tiles along N; counts of bytes and of tiles in 32 bits)
-  if (M > (1 << 24) || N > (1 << 24) || K > (1 << 24) || lda >= (1ll << 40) || ldb >= (1ll << 40)) return MCD_ERR_UNSUPPORTED;
+  if (M > (1 << 24) || N > (1 << 24) || K > (1 << 24) || lda >= (1ll << 36) || ldb >= (1ll << 36) || ldy >= (1ll << 36))
+    return MCD_ERR_UNSUPPORTED;
   const rows::Block a{A, lda, M, K, 1}, b{B, ldb, N, K, 1}, y{Y, ldy, N, M, rows::bytes_of(y_dtype)};
   if (!a.aligned() || !b.aligned() || !y.aligned()) return MCD_ERR_UNSUPPORTED;
-  const rows::Block sa{a_scale, M, 1, M, 4}, sb{b_scale, N, 1, N, 4};
+  if (!rows::aligned_to(a_scale, 4) || !rows::aligned_to(b_scale, 4) || !rows::aligned_to(err, 4)) return MCD_ERR_UNSUPPORTED;
+  const rows::Block sa = rows::values(a_scale, M, 4), sb = rows::values(b_scale, N, 4);
   for (const rows::Block* x : {&a, &b, &sa, &sb})
     if (rows::overlap(y, *x)) return MCD_ERR_INVALID_ARG;
   const tc::Args8 g{a_scale, b_scale, Y, ldy, M, N, K, 0, 1, 0, err};

@@ -212,11 +212,10 @@ extern "C" mcd_status mcd_norm_rows(int32_t n_rows, int32_t width, const void* x
   for (const Block* b : {&in[0], &in[1], &out[0], &out[1]}) {
     if (!b->p) continue;
     if (b->stride < width) return MCD_ERR_INVALID_ARG;
-    if (!b->aligned()) return MCD_ERR_UNSUPPORTED;
+    if (!b->aligned() || !b->fits()) return MCD_ERR_UNSUPPORTED;
   }
-  const Block one_gain{gain, width, 1, width, 4}, scales{k8 ? y_scale : nullptr, n_rows, 1, n_rows, 4};
-  if (gain && !one_gain.aligned()) return MCD_ERR_UNSUPPORTED;
-  if (k8 && (reinterpret_cast<uintptr_t>(y_scale) & 3u)) return MCD_ERR_UNSUPPORTED;
+  const Block one_gain = values(gain, width, 4), scales = values(k8 ? y_scale : nullptr, n_rows, 4);
+  if (!aligned_to(gain, 16) || !aligned_to(scales.p, 4)) return MCD_ERR_UNSUPPORTED;
   for (const Block& o : out) {
     for (const Block& i : in)
       if (overlap(o, i) && !same(o, i)) return MCD_ERR_INVALID_ARG;

@@ -97,7 +97,11 @@ struct Block {
   uintptr_t at() const { return reinterpret_cast<uintptr_t>(p); }
   uintptr_t end() const { return at() + (uintptr_t)(((n_rows - 1) * stride + width) * size); }
   bool aligned() const { return !(at() & 15u) && (n_rows < 2 || stride * size % 16 == 0); }
+  bool fits() const { return n_rows < 2 || stride <= (1ll << 60) / (n_rows * size); }      // (its bytes can be counted)
 };
+// n values of `size` bytes one after another (null: none).
+inline Block values(const void* p, int64_t n, int size) { return {p, n, 1, n, size}; }
+inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline bool same(const Block& a, const Block& b) { return a.p == b.p && a.size == b.size && (a.n_rows < 2 || a.stride == b.stride); }
 // Whether two blocks share a byte.  (Rows of one stride may lie beside each other; of two strides that is not looked into.)
 inline bool overlap(const Block& a, const Block& b) {

@@ -461,15 +461,21 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
     if (rank == 0 && t == 0) give(at.x, 1ull, {1ull, 1u});
     return;
   }
-  // the row's ids that `want` takes (some may have no weight): to each CTA's list, and if there are no more than it holds, all to the
+  // the row's ids that `want` takes (weighed: those of them with weight): to each CTA's list, and if there are no more than it holds, all to the
   // first one's; how many there are
-  auto gather = [&](auto want) {
+  auto gather = [&](bool weighed, auto want) {
     if (t == 0) sm.n_list = 0u;
     __syncthreads();
     each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
       uint32_t on = 0u;
 #pragma unroll
       for (int e = 0; e < 8; ++e) on |= (uint32_t)(e < left && want(v[e])) << e;
+      if (weighed && __any_sync(0xffffffffu, on != 0u)) {
+        uint32_t w[8];
+        weight.eight(v, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) on &= ~((uint32_t)(w[e] == 0u) << e);
+      }
       // (few of a warp's ids, as a rule: one of a lane at a time)
       for (unsigned mask; (mask = __ballot_sync(0xffffffffu, on != 0u)) != 0u; on &= on - 1u) {
         uint32_t at = 0u;
@@ -642,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
   if (has_k && top_k <= n * kGroups) {
     // a rounded quotient can put an id of weight below the point where none should have any: 1e-6 of the logits covers it
     const float near = fmaxf(least, top - 22.f * temp - fabsf(top) * 1e-6f);
-    listed = gather([&](float x) { return x >= near; }) <= (uint32_t)kList;
+    listed = gather(false, [&](float x) { return x >= near; }) <= (uint32_t)kList;
     if (listed) {
       if (rank > 0) return;
       const float span = top - near;
@@ -664,7 +670,9 @@ __global__ void __launch_bounds__(kThreads, 3) sample_kernel(const SampleArgs a)
         cut_in(l, by_mass, target);
         return;
       }
-      gather([&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      // (the bins have counted ids of weight alone; the last ones, and all where a difference of quotients is coarse, hold others
+      // too, which could be too many)
+      gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
       listed = all;
       if (rank > 0 && all) return;
       if (rank == 0) {
@@ -865,7 +873,19 @@ extern "C" mcd_status mcd_sample_rows(int32_t n_rows, int32_t vocab, const void*
   if (n_rows == 0) return MCD_OK;
   if (!logits || !u || !ids || stride < vocab) return MCD_ERR_INVALID_ARG;
   const Block in{logits, stride, n_rows, vocab, bytes_of(dtype)};
-  if (!in.aligned()) return MCD_ERR_UNSUPPORTED;
+  if (!in.aligned() || !in.fits() || !aligned_to(u, 8)) return MCD_ERR_UNSUPPORTED;
+  const void* const fours[] = {temperature, top_k, top_p, min_p, ids, probs, kept, err};
+  for (const void* p : fours)
+    if (!aligned_to(p, 4)) return MCD_ERR_UNSUPPORTED;
+  const Block read[] = {in, values(temperature, n_rows, 4), values(top_k, n_rows, 4), values(top_p, n_rows, 4), values(min_p, n_rows, 4),
+                        values(u, n_rows, 8)};
+  const Block written[] = {values(ids, n_rows, 4), values(probs, n_rows, 4), values(kept, n_rows, 4), values(err, 1, 4)};
+  for (int i = 0; i < 4; ++i) {
+    for (const Block& r : read)
+      if (overlap(written[i], r)) return MCD_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[i], written[j])) return MCD_ERR_INVALID_ARG;
+  }
   const SampleArgs a{logits, stride, vocab, 1, temperature, top_k, top_p, min_p, u, ids, probs, kept, err};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return cuda_status(dtype == MCD_WEIGHT_F32 ? launch_sample<float>(a, n_rows, st) : launch_sample<uint16_t>(a, n_rows, st));

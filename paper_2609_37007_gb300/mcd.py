@@ -546,14 +546,14 @@ def mcd_pages_compact(kv: McdPagedKV, table_in, table_out, start, keep, n_keep, 
 
 # ---- rows between the products (include/mcd_rows.h) and 8-bit products (include/mcd_tc.h) ----
 # The same holds of these: a row's call is shorter than its checks would be with a helper for each.
-def _stride(t, n: int, w: int, what: str) -> int:
-    """Row stride (elements) of a device matrix [n, w] whose rows are contiguous."""
-    if t.shape != (n, w) or not t.is_cuda:
+def _stride(t, shape, n: int, w: int, what: str) -> int:
+    """Row stride (elements) of a device matrix of the shape (n, w) whose rows are contiguous."""
+    if t.shape != shape or not t.is_cuda:
         raise ValueError(f"{what}: a CUDA tensor [{n}, {w}]")
     s, one = t.stride()
     if one != 1 and w != 1:
         raise ValueError(f"{what}: a row's elements are contiguous")
-    return s if n > 1 else max(s, w)
+    return s if n > 1 or s > w else w
 
 
 def _values(t, dtype, what: str, n: int) -> int:
@@ -563,33 +563,33 @@ def _values(t, dtype, what: str, n: int) -> int:
     return t.data_ptr()
 
 
-def _row_dtype(t) -> int:
-    d = t.dtype
-    return 1 if d is _BF16 else 0 if d is _F32 else 3 if d is _E4M3 else _kv_dtype(t)      # MCD_WEIGHT_BF16, _F32, MCD_E4M3
-
-
 def mcd_norm_rows(x, y, residual=None, sum_out=None, gain=None, eps: float = 1e-6, norm: bool = True, y_scale=None, stream=None):
     """y [rows, width] = RMSNorm of x + residual times gain (norm False: without the norm), float32, bfloat16 or float8_e4m3fn
     with a float32 scale per row in y_scale; the sum goes to sum_out.  x, residual and sum_out float32 or bfloat16.  Asynchronous."""
     if _F32 is None:
         _types()
-    n, w = x.shape
+    shape = x.shape
+    n, w = shape
     res = total = scale = None
     rs = ss = kind = 0
     if residual is not None:
-        res, rs, kind = residual.data_ptr(), _stride(residual, n, w, "residual"), _kv_dtype(residual)
+        res, rs, kind = residual.data_ptr(), _stride(residual, shape, n, w, "residual"), 0 if residual.dtype is _F32 else _kv_dtype(residual)
     if sum_out is not None:
-        total, ss, k = sum_out.data_ptr(), _stride(sum_out, n, w, "sum_out"), _kv_dtype(sum_out)
+        k = 0 if sum_out.dtype is _F32 else _kv_dtype(sum_out)
         if res is not None and k != kind:
             raise ValueError("residual and sum_out have one type")
-        kind = k
-    if y_scale is not None:
-        scale = _values(y_scale, _F32, "y_scale", n)
-    elif y.dtype is _E4M3:
-        raise ValueError("8-bit rows need y_scale")
+        total, ss, kind = sum_out.data_ptr(), _stride(sum_out, shape, n, w, "sum_out"), k
+    t = y.dtype
+    if t is _E4M3:
+        if y_scale is None:
+            raise ValueError("8-bit rows need y_scale")
+        scale, t = _values(y_scale, _F32, "y_scale", n), 3      # MCD_E4M3
+    else:
+        t = _kv_dtype(y)
     st = (_lib or load_library()).mcd_norm_rows(
-        n, w, x.data_ptr(), _stride(x, n, w, "x"), _kv_dtype(x), res, rs, total, ss, kind, norm, None if gain is None else _values(gain, _F32, "gain", w),
-        eps, y.data_ptr(), _stride(y, n, w, "y"), _row_dtype(y), scale, None if stream is None else stream.cuda_stream)
+        n, w, x.data_ptr(), _stride(x, shape, n, w, "x"), 0 if x.dtype is _F32 else _kv_dtype(x), res, rs, total, ss, kind, norm,
+        None if gain is None else _values(gain, _F32, "gain", w), eps, y.data_ptr(), _stride(y, shape, n, w, "y"), t, scale,
+        None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_norm_rows", st)
 
@@ -599,9 +599,10 @@ def mcd_sample_rows(logits, u, ids, err, temperature=None, top_k=None, top_p=Non
     per row: temperature, top_p, min_p float32, top_k int32; probs float32 and kept int32 are optional outputs.  Asynchronous."""
     if _F32 is None:
         _types()
-    n, v = logits.shape
+    shape = logits.shape
+    n, v = shape
     st = (_lib or load_library()).mcd_sample_rows(
-        n, v, logits.data_ptr(), _stride(logits, n, v, "logits"), _kv_dtype(logits),
+        n, v, logits.data_ptr(), _stride(logits, shape, n, v, "logits"), _kv_dtype(logits),
         None if temperature is None else _values(temperature, _F32, "temperature", n), None if top_k is None else _values(top_k, _I32, "top_k", n),
         None if top_p is None else _values(top_p, _F32, "top_p", n), None if min_p is None else _values(min_p, _F32, "min_p", n),
         _values(u, _F64, "u", n), _values(ids, _I32, "ids", n), None if probs is None else _values(probs, _F32, "probs", n),
@@ -615,14 +616,13 @@ def mcd_tc_gemm_e4m3(a, b, y, err, a_scale=None, b_scale=None, stream=None):
     of a and of b.  Asynchronous."""
     if _F32 is None:
         _types()
-    m, k = a.shape
-    n = len(b)
-    if a.dtype is not _E4M3 or b.dtype is not _E4M3:
-        raise ValueError("a and b are float8_e4m3fn")
+    (m, k), (n, kb) = a.shape, b.shape
+    if a.dtype is not _E4M3 or b.dtype is not _E4M3 or k != kb:
+        raise ValueError("a [M, K] and b [N, K] are float8_e4m3fn")
     st = (_lib or load_library()).mcd_tc_gemm_e4m3(
-        m, n, k, a.data_ptr(), _stride(a, m, k, "a"), None if a_scale is None else _values(a_scale, _F32, "a_scale", m), b.data_ptr(),
-        _stride(b, n, k, "b"), None if b_scale is None else _values(b_scale, _F32, "b_scale", n), y.data_ptr(), _stride(y, n, m, "y"), _kv_dtype(y),
-        _i32(err, "err"), None if stream is None else stream.cuda_stream)
+        m, n, k, a.data_ptr(), _stride(a, (m, k), m, k, "a"), None if a_scale is None else _values(a_scale, _F32, "a_scale", m), b.data_ptr(),
+        _stride(b, (n, k), n, k, "b"), None if b_scale is None else _values(b_scale, _F32, "b_scale", n), y.data_ptr(),
+        _stride(y, (n, m), n, m, "y"), _kv_dtype(y), _i32(err, "err"), None if stream is None else stream.cuda_stream)
     if st:
         _check("mcd_tc_gemm_e4m3", st)
 

@@ -283,6 +283,19 @@ def test_sample_rows_that_do_not_fit(v):
     check_sample(x, u, temperature=t, top_p=p, min_p=m)
 
 
+@pytest.mark.parametrize("v", [5000, 50000])
+def test_sample_ids_without_weight_beside_the_cut(v):
+    """200 ids of weight 1 (2^31 e^-21.484 = 1.0036) and thousands of weight 0 (e^-21.5) in one step of the histogram; top_p = 1 - 2^-24
+    cuts between the 200."""
+    r = np.random.RandomState(v)
+    x = np.full((4, v), -21.5, np.float32)
+    for i in range(4):
+        x[i, r.permutation(v)[:201]] = -21.484
+        x[i, r.randint(v)] = 0.0
+    check_sample(x, np.array([0.2, 1 - 2.0 ** -40, 0.999999999, 0.5]), top_p=np.full(4, 1 - 2.0 ** -24))
+    check_sample(x, np.array([0.2, 1 - 2.0 ** -40, 0.999999999, 0.5]), top_k=np.full(4, 150), top_p=np.full(4, 1 - 2.0 ** -24))
+
+
 def test_sample_extreme_logits():
     """Temperatures and logits at the ends of fp32: a quotient that overflows means the first of the ranking."""
     x = np.array([[3e38, 1e38, -3e38, 3e38], [1e-40, 0, 2e-40, -1e-40], [-3e38, -3.1e38, -2.9e38, -np.inf], [5, 4, 3, 5]], np.float32)

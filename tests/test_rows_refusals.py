@@ -29,7 +29,7 @@ def norm_call(lib, n=3, w=64, x=P, xs=64, xd=1, res=None, rs=64, sum_out=None, s
     (dict(eps=-1e-6), INVALID), (dict(eps=math.nan), INVALID), (dict(eps=math.inf), INVALID), (dict(yd=3, ys=64, scale=None), INVALID),
     (dict(xd=2), UNSUPPORTED), (dict(xd=3), UNSUPPORTED), (dict(yd=2), UNSUPPORTED), (dict(yd=4), UNSUPPORTED), (dict(res=2 * Q, rd=3), UNSUPPORTED),
     (dict(w=16385, xs=16392, ys=16392), UNSUPPORTED), (dict(x=P + 2), UNSUPPORTED), (dict(xs=65), UNSUPPORTED), (dict(y=Q + 8), UNSUPPORTED),
-    (dict(yd=3, ys=72, scale=2 * Q), UNSUPPORTED), (dict(gain=2 * Q + 4), UNSUPPORTED), (dict(yd=3, scale=2 * Q + 2), UNSUPPORTED),
+    (dict(xs=1 << 62), UNSUPPORTED), (dict(yd=3, ys=72, scale=2 * Q), UNSUPPORTED), (dict(gain=2 * Q + 4), UNSUPPORTED), (dict(yd=3, scale=2 * Q + 2), UNSUPPORTED),
     # outputs over inputs and each other
     (dict(y=P + 16), INVALID), (dict(y=P, ys=72), INVALID), (dict(y=P, yd=0), INVALID), (dict(y=P + 64), INVALID), (dict(sum_out=Q, y=Q), INVALID),
     (dict(sum_out=Q, y=Q + 128), INVALID), (dict(yd=3, y=Q, scale=Q + 64), INVALID), (dict(yd=3, scale=P + 8), INVALID),
@@ -44,14 +44,17 @@ def test_nothing_to_do_is_done(lib):
     assert gemm_call(lib, n=0, b=None) == OK and gemm_call(lib, m=0, a=None) == OK
 
 
-def sample_call(lib, n=3, v=64, x=P, xs=64, xd=0, u=Q, ids=2 * Q, err=3 * Q):
-    return lib.mcd_sample_rows(n, v, x, xs, xd, None, None, None, None, u, ids, None, None, err, None)
+def sample_call(lib, n=3, v=64, x=P, xs=64, xd=0, u=Q, ids=2 * Q, err=3 * Q, temp=None, k=None, p=None, m=None, probs=None, kept=None):
+    return lib.mcd_sample_rows(n, v, x, xs, xd, temp, k, p, m, u, ids, probs, kept, err, None)
 
 
 @pytest.mark.parametrize("bad,want", [
     (dict(n=-1), INVALID), (dict(v=0), INVALID), (dict(x=None), INVALID), (dict(u=None), INVALID), (dict(ids=None), INVALID), (dict(err=None), INVALID),
     (dict(xs=63), INVALID), (dict(xd=2), UNSUPPORTED), (dict(xd=3), UNSUPPORTED), (dict(v=262145, xs=262152), UNSUPPORTED), (dict(x=P + 4), UNSUPPORTED),
-    (dict(xs=66), UNSUPPORTED), (dict(xs=68, xd=1), UNSUPPORTED), (dict(n=(1 << 27) + 1), UNSUPPORTED)])
+    (dict(xs=66), UNSUPPORTED), (dict(xs=68, xd=1), UNSUPPORTED), (dict(n=(1 << 27) + 1), UNSUPPORTED), (dict(xs=1 << 60), UNSUPPORTED),
+    (dict(u=Q + 4), UNSUPPORTED), (dict(ids=2 * Q + 2), UNSUPPORTED), (dict(temp=5 * Q + 1), UNSUPPORTED), (dict(kept=5 * Q + 2), UNSUPPORTED),
+    (dict(ids=P + 256), INVALID), (dict(probs=2 * Q + 8), INVALID), (dict(kept=Q), INVALID), (dict(probs=5 * Q, kept=5 * Q), INVALID),
+    (dict(k=2 * Q), INVALID), (dict(temp=5 * Q, probs=5 * Q), INVALID), (dict(ids=3 * Q), INVALID), (dict(err=P + 4), INVALID)])
 def test_sample_rows_refuses(lib, bad, want):
     assert sample_call(lib, **bad) == want
 
@@ -65,7 +68,8 @@ def gemm_call(lib, m=128, n=16, k=64, a=P, lda=64, sa=None, b=Q, ldb=64, sb=None
     (dict(y=None), INVALID), (dict(err=None), INVALID), (dict(lda=63), INVALID), (dict(ldb=48), INVALID), (dict(ldy=127), INVALID), (dict(y=P), INVALID),
     (dict(y=Q + 512), INVALID), (dict(sa=2 * Q), INVALID), (dict(sb=2 * Q + 1024), INVALID), (dict(yd=2), UNSUPPORTED), (dict(yd=3), UNSUPPORTED),
     (dict(a=P + 8), UNSUPPORTED), (dict(b=Q + 1), UNSUPPORTED), (dict(lda=72), UNSUPPORTED), (dict(ldb=72), UNSUPPORTED), (dict(ldy=130), UNSUPPORTED),
-    (dict(m=(1 << 24) + 1, ldy=1 << 25), UNSUPPORTED), (dict(n=(1 << 24) + 1), UNSUPPORTED), (dict(lda=1 << 40), UNSUPPORTED)])
+    (dict(m=(1 << 24) + 1, ldy=1 << 25), UNSUPPORTED), (dict(n=(1 << 24) + 1), UNSUPPORTED), (dict(lda=1 << 40), UNSUPPORTED),
+    (dict(ldy=1 << 36), UNSUPPORTED), (dict(sa=5 * Q + 2), UNSUPPORTED), (dict(sb=5 * Q + 1), UNSUPPORTED)])
 def test_gemm_refuses(lib, bad, want):
     assert gemm_call(lib, **bad) == want
 
