@@ -296,6 +296,16 @@ def test_sample_ids_without_weight_beside_the_cut(v):
     check_sample(x, np.array([0.2, 1 - 2.0 ** -40, 0.999999999, 0.5]), top_k=np.full(4, 150), top_p=np.full(4, 1 - 2.0 ** -24))
 
 
+@pytest.mark.parametrize("n,v", [(233, 9001), (515, 8193), (58, 70001)])
+def test_sample_more_rows_than_run_together(n, v):
+    """Rows of several CTAs that wait for SMs are taken in an order by their settings, 256 at a time: each one once."""
+    r = np.random.RandomState(n)
+    given = settings(r, n)
+    given["temperature"][:3] = 0.0
+    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), **given)
+    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), top_p=given["top_p"])
+
+
 def test_sample_extreme_logits():
     """Temperatures and logits at the ends of fp32: a quotient that overflows means the first of the ranking."""
     x = np.array([[3e38, 1e38, -3e38, 3e38], [1e-40, 0, 2e-40, -1e-40], [-3e38, -3.1e38, -2.9e38, -np.inf], [5, 4, 3, 5]], np.float32)
