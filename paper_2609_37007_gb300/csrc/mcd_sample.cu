@@ -21,6 +21,7 @@
 #include <cooperative_groups.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "mcd_cache.cuh"
 #include "mcd_rows.cuh"
@@ -445,6 +446,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
   const bool greedy = temp == 0.f || !(fabsf(z_top) <= 3.40282347e38f) || top_k == 1 || top_p <= 0.f;
   const uint32_t w_min = min_p > 0.f ? max(1u, (uint32_t)ceil((double)fminf(min_p, 1.f) * 2147483648.)) : 1u;
   const Weigh weight{temp, __fdiv_rn(1.f, temp), z_top, plain && fabsf(top) < 1e28f};
+  // no id below it has a weight that counts (the margins cover the roundings of quotient, difference and exponential)
+  const float floor_x = top + temp * fmaxf(-22.f, w_min > 1u ? logf(fminf(min_p, 1.f)) - 1e-3f : -22.f) - fabsf(top) * 1e-6f;
 
   bool listed = false;
   // f(on, key, id, weigh) for the CTA's share of the row, or (the first CTA alone) of the list, warp by warp
@@ -490,6 +493,26 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     if (rank == 0 && t == 0) give(at.x, 1ull, {1ull, 1u});
     return;
   }
+  // the CTAs' lists, if the first one's holds them all, to it; how many ids they have
+  auto together = [&] {
+    if (n == 1) return sm.n_list;
+    mine.lo = sm.n_list;
+    tell(3);
+    uint32_t sum = 0u;
+    for (int z = 0; z < n; ++z) sum += sm.told[3][z].lo;
+    if (sum <= (uint32_t)kList) {
+      if (rank > 0) {
+        uint32_t from = 0u;
+        for (int z = 0; z < rank; ++z) from += sm.told[3][z].lo;
+        Shared& first = *cl.map_shared_rank(&sm, 0);
+        for (uint32_t i = t; i < mine.lo; i += kThreads) first.key[from + i] = sm.key[i], first.id[from + i] = sm.id[i], first.w[from + i] = sm.w[i];
+      } else if (t == 0) {
+        sm.n_list = sum;
+      }
+    }
+    cluster_sync();                                         // (the lists have come)
+    return sum;
+  };
   // the row's ids that `want` takes (weighed: those of them with weight): to each CTA's list, and if there are no more than it holds, all to the
   // first one's; how many there are
   auto gather = [&](bool weighed, auto want) {
@@ -531,23 +554,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
         if (i + e < count) sm.w[i + e] = w[e];
     }
     __syncthreads();
-    if (n == 1) return sm.n_list;
-    mine.lo = sm.n_list;
-    tell(3);
-    uint32_t sum = 0u;
-    for (int z = 0; z < n; ++z) sum += sm.told[3][z].lo;
-    if (sum <= (uint32_t)kList) {
-      if (rank > 0) {
-        uint32_t from = 0u;
-        for (int z = 0; z < rank; ++z) from += sm.told[3][z].lo;
-        Shared& first = *cl.map_shared_rank(&sm, 0);
-        for (uint32_t i = t; i < mine.lo; i += kThreads) first.key[from + i] = sm.key[i], first.id[from + i] = sm.id[i], first.w[from + i] = sm.w[i];
-      } else if (t == 0) {
-        sm.n_list = sum;
-      }
-    }
-    cluster_sync();                                         // (the lists have come)
-    return sum;
+    return together();
   };
   // narrows [at.x, at.y], a range of what `of` gives, to the one value where the running sum over descending values reaches the
   // target; in: its sums, as far as they are known
@@ -671,7 +678,58 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
   // (top_p < 1 and a mass below 2^50: the product is at most the mass)
   auto need_of = [&](unsigned long long mass) { return min(max(1ull, (unsigned long long)ceil((double)top_p * (double)mass)), mass); };
 
-  bool p_done = false;
+  // Sums of W, of blocks of 256 ids and of all, of the row's ids before the cut; or, with a cut that is still to be found in bin l.bin,
+  // of those in the bins above, while that one's ids go to the CTA's list.
+  Tally sums{0ull, 0u};
+  auto sum_row = [&](auto is_open, uint32_t bin) {
+    constexpr bool open = decltype(is_open)::value;
+    if (t == 0) sm.n_list = 0u;
+    __syncthreads();
+    const float from = fmaxf(floor_x, logit_of(cut.key));
+    int i = warp;
+    each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
+      Tally y{0ull, 0u};
+      float most = v[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) most = fmaxf(most, v[e]);
+      if (__any_sync(0xffffffffu, open ? bin_of(most) >= bin : most >= from)) {
+        uint32_t w[8], on = 0u;
+        weight.eight(v, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          bool in = e < left && w[e] >= w_min;
+          if constexpr (open) {
+            const uint32_t b = bin_of(v[e]);
+            on |= (uint32_t)(e < left && w[e] > 0u && b == bin) << e;
+            in = in && b > bin;
+          } else {
+            in = in && logit_before_cut(v[e], (uint32_t)(id + e));
+          }
+          y.mass += in ? w[e] : 0u, y.count += in;
+        }
+        y.mass = warp_sum36(y.mass);                   // (eight of 2^31 at most)
+        if constexpr (open) {
+          for (unsigned mask; (mask = __ballot_sync(0xffffffffu, on != 0u)) != 0u; on &= on - 1u) {
+            uint32_t at = 0u;
+            if (lane == 0) at = atomicAdd(&sm.n_list, (uint32_t)__popc(mask));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(mask & ((1u << lane) - 1u));
+            const int first = __ffs(on) - 1;
+            float x = v[0];
+            uint32_t own = w[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) x = e == first ? v[e] : x, own = e == first ? w[e] : own;
+            if (on != 0u && at < (uint32_t)kList) sm.key[at] = key_of(x), sm.id[at] = (uint32_t)(id + first), sm.w[at] = own;
+          }
+        }
+      }
+      if (lane == 0) sm.block[i] = y.mass, sums.mass += y.mass;
+      sums.count += y.count;
+      i += kWarps;
+    });
+    __syncthreads();
+  };
+
+  bool p_done = false, summed = false;
   if (has_k && top_k <= n * kGroups) {
     // a rounded quotient can put an id of weight below the point where none should have any: 1e-6 of the logits covers it
     const float near = fmaxf(least, top - 22.f * temp - fabsf(top) * 1e-6f);
@@ -691,7 +749,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     has_k = has_k && (uint32_t)top_k < cut.in.count;
     unsigned long long target = has_k ? (unsigned long long)top_k : need_of(cut.in.mass);
     // (a bin's ids to the list, or all down to it: the first CTA alone finds the cut and, in the first case, tells the others)
-    auto find = [&](const Level l, bool by_mass) {
+    auto find = [&](const Level l, bool by_mass, bool last) {
+      if (last && w_min > 1u && bin_of(floor_x) > l.bin) return;      // (min_p leaves less than the cut)
       const bool all = l.above.count + l.at.count <= (uint32_t)kList;
       if (!all && l.at.count > (uint32_t)kList) {
         cut_in(l, by_mass, target);
@@ -699,7 +758,15 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
       }
       // (the bins have counted ids of weight alone; the last ones, and all where a difference of quotients is coarse, hold others
       // too, which could be too many)
-      gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      uint32_t own = 0u;
+      if (!all && last) {
+        sum_row(std::true_type{}, l.bin);
+        own = sm.n_list;
+        together();
+        summed = true;
+      } else {
+        gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      }
       listed = all;
       if (rank > 0 && all) return;
       if (rank == 0) {
@@ -713,15 +780,24 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
       }
       meet();
       cut = sm.cut;
+      if (summed) {
+        for (uint32_t i = t; i < own; i += kThreads) {
+          const uint32_t w = sm.w[i];
+          if (w >= w_min && before_cut(sm.key[i], sm.id[i])) {
+            atomicAdd(&sm.block[(sm.id[i] - (uint32_t)lo) >> 8], (unsigned long long)w);
+            sums.mass += w, ++sums.count;
+          }
+        }
+      }
       meet();
     };
     if (has_k || has_p) {
-      find(crossing(sm, b, !has_k, target), !has_k);
+      find(crossing(sm, b, !has_k, target), !has_k, !(has_k && has_p));
       if (listed && rank > 0) return;
       p_done = !has_k;
       if (has_k && has_p && !listed) {
         target = need_of(cut.in.mass);
-        find(crossing(sm, b, true, target), true);
+        find(crossing(sm, b, true, target), true, true);
         if (listed && rank > 0) return;
         p_done = true;
       }
@@ -730,24 +806,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
 
   // ---- the draw
   if (!listed) {
-    // from the row: blocks of 256 ids
-    Tally x{0ull, 0u};
-    int i = warp;
-    each_eight(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
-      Tally y{0ull, 0u};
-      uint32_t w[8];
-      weight.eight(v, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool on = e < left && w[e] >= w_min && logit_before_cut(v[e], (uint32_t)(id + e));
-        y.mass += on ? w[e] : 0u, y.count += on;
-      }
-      y.mass = warp_sum36(y.mass);                     // (eight of 2^31 at most)
-      if (lane == 0) sm.block[i] = y.mass, x.mass += y.mass;
-      x.count += y.count;
-      i += kWarps;
-    });
-    mine.sum = block_sum(sm, x);
+    if (!summed) sum_row(std::false_type{}, 0u);
+    mine.sum = block_sum(sm, sums);
     tell(1);
     Tally in{0ull, 0u};
     unsigned long long ahead = 0ull;
