@@ -178,18 +178,12 @@ struct Weigh {
 #pragma unroll
       for (int e = 0; e < 4; ++e) z[e] = pack2(__fdiv_rn(v[2 * e], temp), __fdiv_rn(v[2 * e + 1], temp));
     }
-    // (one at a time: ptxas makes a mul.rn.f32x2 and the add.rn.f32x2 that takes it one operation, rounded once)
-    auto plus = [](uint64_t a, float b) {
-      float x, y;
-      unpack2(a, x, y);
-      return pack2(__fadd_rn(x, b), __fadd_rn(y, b));
-    };
-    auto sum = [](uint64_t a, uint64_t b) {
-      float x, y, u, v;
-      unpack2(a, x, y);
-      unpack2(b, u, v);
-      return pack2(__fadd_rn(x, u), __fadd_rn(y, v));
-    };
+    // (times one: ptxas makes a mul.rn.f32x2 and an add.rn.f32x2 that takes it one operation, rounded once)
+    float alone = 1.f;
+    asm("" : "+f"(alone));
+    const uint64_t ones = both(alone);
+    auto sum = [&](uint64_t a, uint64_t b) { return fma2(a, ones, b); };
+    auto plus = [&](uint64_t a, float b) { return fma2(a, ones, both(b)); };
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float d[2], y[2], p[2];
@@ -613,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     if (t == 0) sm.n_few = 0u;
     __syncthreads();
     each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
-      on = on && want(key, id);
+      on = on && want(key, id, weigh());
       const unsigned mask = __ballot_sync(0xffffffffu, on);
       if (!mask) return;
       uint32_t at = 0u;
@@ -642,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
       fine = true;
     }
     if (listed && l.at.count <= (uint32_t)kFew) {
-      const int few = gather_few(member);
+      const int few = gather_few([&](uint32_t key, uint32_t id, uint32_t) { return member(key, id); });
       if (t < few) {
         const uint4 me = sm.few[t];
         const uint32_t key = me.x, id = me.y, w = me.z;
@@ -871,7 +865,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     p_done = true;
   }
   if (cut.in.count <= (uint32_t)kFew) {
-    const int few = gather_few(before_cut);
+    const int few = gather_few([&](uint32_t key, uint32_t id, uint32_t) { return before_cut(key, id); });
     const unsigned long long need = has_p && !p_done ? need_of(cut.in.mass) : ~0ull;
     uint32_t key = 0u, id = 0u, w = 0u;
     if (t < few) {
@@ -902,16 +896,31 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     }
     return;
   }
-  Tally in = cut.in;
-  if (w_min > 1u) {
-    Tally x{0ull, 0u};
+  // (256 parts of the ids, and the few of one, as a rule)
+  const int part = max(0, 24 - __clz(V - 1));
+  const Bins b = count_bins(sm, 1, {0ull, 0u}, [&](auto) {
     each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
-      const uint32_t w = on && before_cut(key, id) ? weigh() : 0u;
-      if (w >= w_min) x.mass += w, ++x.count;
+      const uint32_t w = weigh();
+      hist_add_one(sm, on && w >= w_min && before_cut(key, id), 255u - (id >> part), w);
     });
-    in = block_sum(sm, x);
-  }
+  });
+  const Tally in = bins_sum(sm, b);
   const unsigned long long drawn = min((unsigned long long)floor(u * (double)in.mass), in.mass - 1);
+  const Level l = crossing(sm, b, true, drawn + 1);
+  if (l.at.count <= (uint32_t)kFew) {
+    const int few = gather_few([&](uint32_t key, uint32_t id, uint32_t w) { return w >= w_min && 255u - (id >> part) == l.bin && before_cut(key, id); });
+    if (t < few) {
+      const uint32_t id = sm.few[t].y, w = sm.few[t].z;
+      unsigned long long before = l.above.mass;
+#pragma unroll 8
+      for (int j = 0; j < few; ++j) {
+        const uint4 o = sm.few[j];
+        before += o.y < id ? o.z : 0u;
+      }
+      if (before <= drawn && drawn < before + w) give(id, w, in);
+    }
+    return;
+  }
   auto of = [&](uint32_t key, uint32_t id) { return before_cut(key, id) ? from_id(id) : 0xffffffffu; };
   const Level p = narrow(extent(of), true, drawn + 1, {0ull, 0u}, in, w_min, of);
   if (t == 0) give(from_id(p.bin), p.at.mass, in);
