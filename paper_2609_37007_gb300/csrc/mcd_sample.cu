@@ -663,7 +663,19 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
     cut.key = p.bin;
     if (ties < p.at.count) {
       auto tie = [&](uint32_t key, uint32_t id) { return key == cut.key && (key > old.key || id <= old.id) ? from_id(id) : 0xffffffffu; };
-      cut.id = from_id(narrow(extent(tie), false, ties, {0ull, 0u}, {0ull, 0u}, 1u, tie).bin);
+      if (listed && p.at.count <= (uint32_t)kFew) {
+        const int few = gather_few([&](uint32_t key, uint32_t id, uint32_t) { return tie(key, id) != 0xffffffffu; });
+        if (t < few) {
+          const uint32_t id = sm.few[t].y;
+          uint32_t before = 0u;
+          for (int j = 0; j < few; ++j) before += sm.few[j].y < id;
+          if (before == ties - 1u) sm.cut.id = id;
+        }
+        __syncthreads();
+        cut.id = sm.cut.id;
+      } else {
+        cut.id = from_id(narrow(extent(tie), false, ties, {0ull, 0u}, {0ull, 0u}, 1u, tie).bin);
+      }
     } else if (cut.key > old.key) {
       cut.id = 0xffffffffu;
     }
@@ -783,7 +795,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) sample_kernel(const SampleAr
           }
         }
       }
-      meet();
     };
     if (has_k || has_p) {
       find(crossing(sm, b, !has_k, target), !has_k, !(has_k && has_p));
