@@ -13,7 +13,7 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libmcd.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 SOURCES = ["mcd_api.cu", "mcd_frame.cu", "mcd_static.cu", "mcd_outer.cu", "mcd_batch.cu", "mcd_tcgemm.cu", "mcd_rope.cu",
-           "mcd_pages.cu", "mcd_attn.cu", "mcd_attn_chunk.cu", "mcd_rows.cu", "mcd_sample.cu", "mcd_gemm8.cu"]
+           "mcd_pages.cu", "mcd_attn.cu", "mcd_attn_chunk.cu", "mcd_rows.cu", "mcd_sample.cu", "mcd_sample_bf16.cu", "mcd_gemm8.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-cudart", "shared",
          "-I" + os.path.join(ROOT, "include")]
