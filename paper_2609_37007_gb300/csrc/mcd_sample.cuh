@@ -7,7 +7,7 @@
 // their keys first).  The draw is the same on ids in ascending order, its target a sum of weights.
 //
 // A cluster of CTAs takes a row and reads it for the maximum.  Then one of three ways:
-//   top_k up to the cluster's half warps: so many ids are not below the least of the half warps' maxima; what is not goes to a
+//   top_k up to 128: of as many groups of threads, so many ids are not below the least of the groups' maxima; what is not goes to a
 //     list in the first CTA's shared memory, and the first CTA goes on alone;
 //   top_k otherwise, top_p: the histogram is made from the row, by all CTAs; the ids of the bins down to the crossing one go to the list,
 //     as above; where they are too many, those of the crossing bin alone, and the draw is from the row;
@@ -55,7 +55,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kMaxWarps = 16;
-constexpr int kGroups = 16;            // groups of threads, whose maxima bound the largest ids
+constexpr int kMostGroups = 128;       // groups of threads, whose maxima bound the largest ids
 constexpr int kMaxCluster = 8, kPerSm = 4;
 constexpr int kList = 3200;            // ids of the list
 constexpr int kFew = 128;              // ids whose order is found by comparing all with all
@@ -102,7 +102,8 @@ struct Shared {
   uint32_t n_list, n_few;
   Told told[4][kMaxCluster];           // of the maximum, of sums, of extents
   Tally red[kMaxWarps];
-  float fred[kGroups];
+  float fred[2][kMaxWarps];
+  int flags[kMaxWarps];
   uint32_t ured[2][kMaxWarps];
   uint32_t bin;
   Tally above, at;
@@ -352,8 +353,8 @@ template <class T, bool kAlone, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kPerSm) sample_kernel(const SampleArgs a) {
   __shared__ Shared shared;
   Shared& sm = shared;
-  constexpr int kWarps = kThreads / 32, kGroup = kThreads / kGroups;
-  static_assert(kThreads >= 256 && kWarps <= kMaxWarps && (kGroup == 16 || kGroup == 32), "a thread a bin; groups within warps");
+  constexpr int kWarps = kThreads / 32;
+  static_assert(kThreads >= 256 && kWarps <= kMaxWarps, "a thread a bin");
   cg::cluster_group cl = cg::this_cluster();
   const int n = kAlone ? 1 : a.cluster, rank = n > 1 ? (int)cl.block_rank() : 0, t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int V = a.vocab, per = ((V + n - 1) / n + 7) / 8 * 8, lo = min(V, rank * per), hi = min(V, lo + per);
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     if (on) {
       const float p = a.top_p ? __ldg(a.top_p + from + t) : 1.f;
       const int k = a.top_k ? __ldg(a.top_k + from + t) : 0;
-      kind = (a.temperature && __ldg(a.temperature + from + t) == 0.f) || k == 1 || p <= 0.f ? 2 : p < 1.f && (k <= 0 || k > n * kGroups) ? 0 : 1;
+      kind = (a.temperature && __ldg(a.temperature + from + t) == 0.f) || k == 1 || p <= 0.f ? 2 : p < 1.f && (k <= 0 || k > kMostGroups) ? 0 : 1;
     }
     uint32_t at = 0u;
 #pragma unroll
@@ -411,13 +412,21 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
         odd |= size - 0x0e000000u >= 0x61000000u && size != 0u && size != 0x7f800000u;
       }
     });
-#pragma unroll
-    for (int w = kGroup / 2; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
-    if (t % kGroup == 0) sm.fred[t / kGroup] = most;
-    mine.bad = __syncthreads_or(bad);
-    mine.odd = __syncthreads_or(odd);
+    // (as few groups as there must be: a list of k ln k ids, about)
+    int group = 32;
+    while (group > 1 && n * (kThreads / group) < top_k && n * (kThreads / group) < kMostGroups) group /= 2;
+    for (int w = group / 2; w; w >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
+    const uint32_t key = key_of(most);
+    const float warp_top = logit_of(__reduce_max_sync(0xffffffffu, key)), warp_least = logit_of(__reduce_min_sync(0xffffffffu, key));
+    const int flags = (int)__any_sync(0xffffffffu, bad) | (int)__any_sync(0xffffffffu, odd) << 1;
+    if (lane == 0) sm.fred[0][warp] = warp_top, sm.fred[1][warp] = warp_least, sm.flags[warp] = flags;
+    __syncthreads();
     mine.top = -INFINITY, mine.least = INFINITY;
-    for (int i = 0; i < kGroups; ++i) mine.top = fmaxf(mine.top, sm.fred[i]), mine.least = fminf(mine.least, sm.fred[i]);
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) {
+      mine.top = fmaxf(mine.top, sm.fred[0][i]), mine.least = fminf(mine.least, sm.fred[1][i]);
+      mine.bad |= sm.flags[i] & 1, mine.odd |= sm.flags[i] >> 1;
+    }
   }
   // (every CTA's `mine` to all)
   auto tell = [&](int what) {
@@ -746,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
   };
 
   bool p_done = false, summed = false;
-  if (has_k && top_k <= n * kGroups) {
+  if (has_k && top_k <= kMostGroups) {
     // a rounded quotient can put an id of weight below the point where none should have any: 1e-6 of the logits covers it
     const float near = fmaxf(least, top - 22.f * temp - fabsf(top) * 1e-6f);
     listed = gather(false, [&](float x) { return x >= near; }) <= (uint32_t)kList;
@@ -947,11 +956,11 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
   if (t == 0) give(from_id(p.bin), p.at.mass, in);
 }
 
-// CTAs of a row: enough that each has kSlice ids at most.
-constexpr int kSlice = 8192;
-int cluster_for(int vocab) {
+// CTAs of a row: enough that each has 8,192 ids at most; 4,096 where there are so few rows that all have SMs of their own (8 rows of
+// 16,384, top_p 0.9: 17.9 -> 15.6 us, k = 50 11.8 -> 10.4; 1,000 rows of 32,768 would take 197 us instead of 129).
+int cluster_for(int vocab, long long n_rows) {
   int n = 1;
-  while (n < kMaxCluster && vocab > n * kSlice) n *= 2;
+  while (n < kMaxCluster && (vocab > n * 8192 || (vocab > n * 4096 && n_rows * 2 * n <= paged::sm_count()))) n *= 2;
   return n;
 }
 
@@ -959,10 +968,10 @@ int cluster_for(int vocab) {
 
 template <class T>
 cudaError_t launch_sample(SampleArgs a, int n_rows, cudaStream_t st) {
-  a.cluster = cluster_for(a.vocab);
+  a.cluster = cluster_for(a.vocab, n_rows);
   a.n_rows = n_rows;
   // Rows that wait for SMs: those that take 45 us go first, those of 20 fill the ends (96 rows of 131,072: 52 us against 68 in their
-  // own order; 400: 173 against 195).  Where all run at a time it would only cost the look at the settings.
+  // own order; 400: 173 against 195, measured with three CTAs an SM).  Where all run at a time it would only cost the look at the settings.
   a.ordered = (long long)n_rows * a.cluster > kPerSm * paged::sm_count();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_rows * a.cluster);

@@ -296,14 +296,27 @@ def test_sample_ids_without_weight_beside_the_cut(v):
     check_sample(x, np.array([0.2, 1 - 2.0 ** -40, 0.999999999, 0.5]), top_k=np.full(4, 150), top_p=np.full(4, 1 - 2.0 ** -24))
 
 
-@pytest.mark.parametrize("n,v", [(233, 9001), (515, 8193), (58, 70001)])
-def test_sample_more_rows_than_run_together(n, v):
+@pytest.mark.parametrize("n,v,dtype", [(233, 9001, "f32"), (515, 8193, "f32"), (58, 70001, "f32"), (90, 70001, "bf16"), (200, 20001, "bf16"), (60, 20001, "f32")])
+def test_sample_more_rows_than_run_together(n, v, dtype):
     """Rows of several CTAs that wait for SMs are taken in an order by their settings, 256 at a time: each one once."""
     r = np.random.RandomState(n)
     given = settings(r, n)
     given["temperature"][:3] = 0.0
-    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), **given)
-    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), top_p=given["top_p"])
+    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), dtype=dtype, **given)
+    check_sample((2.5 * r.randn(n, v)).astype(np.float32), r.rand(n), dtype=dtype, top_p=given["top_p"])
+
+
+@pytest.mark.parametrize("v", [300, 2048, 8192, 8193, 16385, 40000, 140000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_min_p_beside_top_p(v, dtype):
+    """min_p that leaves less than the cut, more, and as much, with sets from one id to all."""
+    r = np.random.RandomState(v)
+    n = 24
+    p, m = np.repeat([0.05, 0.5, 0.9, 0.999], 6), np.tile([0.0, 1e-9, 1e-4, 0.02, 0.3, 1.0], 4)
+    for spread, t in ((0.3, 1.0), (3.0, 0.9), (3.0, 8.0)):
+        x = (spread * r.randn(n, v)).astype(np.float32)
+        check_sample(x, r.rand(n), dtype=dtype, temperature=np.full(n, t), top_p=p, min_p=m)
+        check_sample(x, r.rand(n), dtype=dtype, temperature=np.full(n, t), top_k=np.tile([129, 5000, 0], 8), top_p=p, min_p=m)
 
 
 def test_sample_extreme_logits():
