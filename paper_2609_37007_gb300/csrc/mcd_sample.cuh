@@ -10,14 +10,15 @@
 //   top_k up to 128: of as many groups of threads, so many ids are not below the least of the groups' maxima; what is not goes to a
 //     list in the first CTA's shared memory, and the first CTA goes on alone;
 //   top_k otherwise, top_p: the histogram is made from the row, by all CTAs; the ids of the bins down to the crossing one go to the list,
-//     as above; where they are too many, those of the crossing bin alone, and the draw is from the row;
+//     as above; where they are too many, those of the crossing bin alone, while the bins above are summed up, and the draw is from
+//     the row.  Where min_p leaves nothing below the crossing bin there is no cut to find;
 //   neither: the draw is from the row: sums of W of blocks of 256 ids, the block in which the target is crossed, the id.
 // Order never changes a result: whole numbers add up to the same sum.
 //
 // What bounds it: weights, about 30 operations each (the definition rounds every product and sum), barriers of the cluster (2,000
-// cycles each) and chains of small steps.  One row of 2,048, k = 50: 7 us on the GPU; of 131,072: 16 us, with top_p alone and 20,000
-// ids left 46.  128 rows of 2,048 with mixed settings 15.5 us, 96 of 131,072 (bf16) 70: the rows with large sets, a fifth, are
-// waited for.  Clusters: a CTA has 8,192 ids of a row, or an eighth of it.
+// cycles each) and chains of small steps.  One row of 2,048, k = 50: 6 us on the GPU; of 131,072: 13 us, with top_p alone and 30,000
+// ids left 28 (35 of 8 rows).  128 rows of 2,048 with mixed settings 12.3 us, 96 of 131,072 (bf16) 47 to 52: as long as the rows with
+// large sets, a fifth, take beside others.
 #pragma once
 #include <cooperative_groups.h>
 
@@ -692,6 +693,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
         }
         __syncthreads();
         cut.id = sm.cut.id;
+        __syncthreads();
       } else {
         cut.id = from_id(narrow(extent(tie), false, ties, {0ull, 0u}, {0ull, 0u}, 1u, tie).bin);
       }
