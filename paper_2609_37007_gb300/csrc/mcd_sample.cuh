@@ -574,7 +574,11 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
   // target; in: its sums, as far as they are known
   auto narrow = [&](uint2 at, bool by_mass, unsigned long long target, Tally above, Tally in, uint32_t least_w, auto of) {
     Level l{0u, above, in};
-    while (at.x != at.y) {
+    for (int rounds = 0; at.x != at.y; ++rounds) {
+      if (rounds > 4 || at.x > at.y) {                 // (eight bits a round; a set without the target would be a fault of this kernel)
+        if (rank == 0 && t == 0) atomicCAS(a.err, 0, (int)MCD_ERR_TIMEOUT);
+        break;
+      }
       const int bits = 32 - __clz(at.y - at.x), shift = bits > 8 ? bits - 8 : 0;
       const Bins b = count_bins<kThreads>(sm, listed ? 1 : n, l.above, [&](auto add) {
         each([&](bool on, uint32_t key, uint32_t id, auto weigh) {
@@ -585,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
         });
       });
       l = crossing(sm, b, by_mass, target);
-      const uint32_t from = at.x + (l.bin << shift), to = min(at.y, from + ((1u << shift) - 1u));
+      const uint32_t from = at.x + (l.bin << shift), to = from + min(at.y - from, (1u << shift) - 1u);
       at = from == to ? make_uint2(from, to) : extent([&](uint32_t key, uint32_t id) {
         const uint32_t x = of(key, id);
         return x >= from && x <= to ? x : 0xffffffffu;
@@ -643,7 +647,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     const Cut old = cut;
     Level l = coarse;
     bool fine = false;
-    auto part_of = [&](float x) { return 255u - (uint32_t)min(255, max(0, (int)(((top - x) * scale - (float)(255u - coarse.bin)) * 256.f))); };
+    auto part_of = [&](float x) { return 255u - (uint32_t)min(255, max(0, (int)(__fsub_rn(__fmul_rn(top - x, scale), (float)(255u - coarse.bin)) * 256.f))); };
     auto member = [&](uint32_t key, uint32_t id) {
       const float x = logit_of(key);
       return (key > old.key || (key == old.key && id <= old.id)) && bin_of(x) == coarse.bin && (!fine || part_of(x) == l.bin);
