@@ -66,7 +66,8 @@ mcd_status mcd_norm_rows(int32_t n_rows, int32_t width, const void* x, int64_t x
  *   probs        dev float [n_rows], optional: W / M of the drawn id
  *   kept         dev int32 [n_rows], optional: how many ids were left
  *   err          dev int32, zeroed by the caller: MCD_ERR_INVALID_ARG when a row has a NaN, +inf or nothing but -inf, or a
- *                setting that is NaN or out of its range; such a row has id -1, probability 0 and 0 ids left
+ *                setting that is NaN or out of its range; such a row has id -1, probability 0 and 0 ids left;
+ *                MCD_ERR_TIMEOUT if a search gave up (a fault of the library: the row's result is not to be used)
  * Rows are 16-byte aligned, vocab is at most 262,144 (MCD_ERR_UNSUPPORTED otherwise).  Outputs and err overlap nothing
  * (MCD_ERR_INVALID_ARG).  No rows: MCD_OK. */
 mcd_status mcd_sample_rows(int32_t n_rows, int32_t vocab, const void* logits, int64_t stride, int32_t dtype,
