@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
   // f(on, key, id, weigh) for the CTA's share of the row, or (the first CTA alone) of the list, warp by warp
   auto each = [&](auto f) {
     if (listed) {
-      const int count = (int)sm.n_list;
+      const int count = min((int)sm.n_list, kList);
       for (int i = t & ~31; i < count; i += kThreads) {
         const int j = min(i + lane, count - 1);
         f(i + lane < count && sm.w[j] > 0u, sm.key[j], sm.id[j], [&] { return sm.w[j]; });
@@ -607,8 +607,9 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     return x > c || (x == c && id <= cut.id);
   };
   auto before_cut = [&](uint32_t key, uint32_t id) { return key > cut.key || (key == cut.key && id <= cut.id); };
-  // steps of the histograms: from the maximum down to where W is 0 (2^31 e^-21.5 < 1), or to the list's end
-  float scale = 255.f / (22.f * temp);
+  // steps of the histograms: from the maximum down to where W is 0 (2^31 e^-21.5 < 1), or to the list's end.  (22 T would leave fp32's
+  // range from 1.5e37 on, and 0 times -inf's distance, NaN, put hidden ids beside the maximum; a tiny T's quotient leaves it too)
+  float scale = fminf(255.f / 22.f / temp, 3.40282347e38f);
   auto bin_of = [&](float x) { return 255u - (uint32_t)min(255, (int)((top - x) * scale)); };
   auto key_bins = [&] {
     return count_bins<kThreads>(sm, listed ? 1 : n, {0ull, 0u}, [&](auto) {
@@ -717,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     if (t == 0) sm.n_list = 0u;
     __syncthreads();
     const float from = fmaxf(floor_x, logit_of(cut.key));
+    sums = {0ull, 0u};
     int i = warp;
     each_eight<T, kThreads>(row, lo, hi, [&](int id, int left, const float (&v)[8]) {
       Tally y{0ull, 0u};
@@ -768,7 +770,7 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     if (listed) {
       if (rank > 0) return;
       const float span = top - near;
-      scale = span > 0.f ? 255.f / span : 0.f;
+      scale = span > 0.f ? fminf(255.f / span, 3.40282347e38f) : 0.f;
       const Bins b = key_bins();
       cut.in = bins_sum(sm, b);
       if ((uint32_t)top_k < cut.in.count) cut_in(crossing(sm, b, false, top_k), false, top_k);
@@ -788,15 +790,20 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
         return;
       }
       // (the bins have counted ids of weight alone; the last ones, and all where a difference of quotients is coarse, hold others
-      // too, which could be too many)
-      uint32_t own = 0u;
+      // too, which could be too many: so can all of a T below 3e-38, whose first bin is wider than what has weight)
+      uint32_t own = 0u, held;
       if (!all && last) {
         sum_row(std::true_type{}, l.bin);
         own = sm.n_list;
-        together();
+        held = together();
         summed = true;
       } else {
-        gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+        held = gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      }
+      if (held > (uint32_t)kList) {                    // (the list has not come together: from the row)
+        summed = false;
+        cut_in(l, by_mass, target);
+        return;
       }
       listed = all;
       if (rank > 0 && all) return;
