@@ -451,6 +451,7 @@ __global__ void __launch_bounds__(kCThreads, 1)
       if (j < early) {                                 // in front of every window: zeros; in front of some: looked at
         const int sinks = min(max(a.sinks - k0, 0), end), none = min(max(lows.from - k0, sinks), end), all = min(max(lows.to - k0, none), end);
         clear_keys(sinks, none);
+        look_at(min(chunk, sinks), sinks);             // (new rows among the sinks: causality or the mask hides them from some)
         look_at(none, all);
         look_at(max(all, min(chunk, end)), end);
       } else {
