@@ -50,7 +50,8 @@ mcd_status mcd_tc_gemm_tiled(int32_t M, int32_t N, int32_t K, int32_t bn, const 
                              float* Y, int32_t* err, void* stream);
 
 /* Y[n][m] = a_scale[m] * b_scale[n] * sum_k A[m][k] * B[n][k] for m < M, n < N: 8-bit operands (e4m3, the type and the row
- * scales of mcd_norm_rows), products and sums as with bf16 in fp32, one rounding to Y.
+ * scales of mcd_norm_rows), products and sums as with bf16 in fp32; the sum times a_scale, that times b_scale, each in fp32 (what leaves
+ * its range on the way is lost), one rounding to Y.
  *   A        dev [M][lda] (weights), B dev [N][ldb] (rows), K bytes used of each row
  *   a_scale  dev float [M], b_scale dev float [N]; NULL: ones
  *   Y        dev [N][ldy], y_dtype MCD_WEIGHT_F32 or MCD_WEIGHT_BF16

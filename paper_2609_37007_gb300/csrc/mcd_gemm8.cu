@@ -103,8 +103,9 @@ template <class T>
 __device__ __forceinline__ void store4_scaled(const Args8& g, int n, int m, float4 v) {
   const float sb = g.b_scale ? __ldg(g.b_scale + n) : 1.f;
   float x[4] = {v.x, v.y, v.z, v.w};
+  // (a's scale, then b's, as drain does it: their product may leave fp32's range where the result does not)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] *= (g.a_scale && m + e < g.M ? __ldg(g.a_scale + m + e) : 1.f) * sb;
+  for (int e = 0; e < 4; ++e) x[e] = x[e] * (g.a_scale && m + e < g.M ? __ldg(g.a_scale + m + e) : 1.f) * sb;
   T* y = static_cast<T*>(g.y) + n * g.ldy + m;
   if (m + 4 <= g.M) {
     paged::store4(y, make_float4(x[0], x[1], x[2], x[3]));
