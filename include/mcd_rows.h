@@ -28,7 +28,8 @@ enum { MCD_E4M3 = 3 };
  * (v comes from the unrounded r), sums are fp32.  With y_dtype MCD_E4M3 the row has a scale,
  * s = max(max |v| / 448, 2^-126), and y = v / s to the nearest value: y * s stands for v.  A row that holds an infinity
  * or NaN has, with `norm`, no finite v, and in 8 bits no finite y * s; nor has, with `norm`, one whose sum of squares
- * leaves fp32's range.  Other rows are not touched by it.
+ * is above fp32's range (squares below it are lost: with eps 0, values below 1e-19).  Other rows are not touched by it.
+ * The gain is multiplied last: r * gain may leave fp32's range where v does not.
  *   x          dev [n_rows][x_stride], x_dtype MCD_WEIGHT_F32 or MCD_WEIGHT_BF16
  *   residual, sum   dev [n_rows][stride], res_dtype likewise.  residual NULL: r = x (res_dtype is sum's).  sum
  *              NULL: not stored

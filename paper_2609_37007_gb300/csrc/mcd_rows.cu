@@ -1,11 +1,11 @@
 // mcd_norm_rows (include/mcd_rows.h): residual sum, RMSNorm and rounding of rows, to 8 bits with a scale too.
 //
 // The mathematics, per row of n elements: r = x + residual; q = sum r^2, i = 1 / sqrt(q / n + eps), v = r i gain.  The scale of
-// 8 bits is max |v| / 448 = i max |r gain| / 448, so that q and the maximum are found in one pass and joined once; the row
-// stays in registers between its load and its store.
+// 8 bits is max |v| / 448 = i max |r gain| / 448, so that q and the maximum are found in one pass and joined once (a row whose
+// r gain leaves fp32's range is looked at again); the row stays in registers between its load and its store.
 // What bounds it: one read of x and the residual, one write of the sum and of y; for a few rows the chain load -> join -> store.
-// 30,011 rows of 4,096, bf16 in, sum and residual, 8 bits out: 154 us, 5.6 TB/s (0.84 of a copy; bf16 out 162, fp32 sums 228 us
-// or 7.0 TB/s).  A thread has 8 or 16 elements and a row as many threads as that takes, so that the SM's 2,048 threads have
+// 30,011 rows of 4,096, bf16 in, sum and residual, 8 bits out: 154 us, 5.6 TB/s (0.84 of a copy; bf16 out 161, fp32 sums and out
+// 257 us or 6.7 TB/s).  A thread has 8 or 16 elements and a row as many threads as that takes, so that the SM's 2,048 threads have
 // 64 bytes each on their way: 4,096 elements on 512 threads 156, on 256 of two chunks 157, on 128 of four 173 us; 1,024 on a warp
 // of four chunks 89 against 72.  CTAs that stay and load the next row under the join took 296 (64 registers: half the threads).
 #include <cmath>
@@ -64,9 +64,9 @@ __device__ __forceinline__ void store8(void* base, long long row, long long stri
 }
 
 // A team of kTeam threads takes a row, thread t its chunks t, t + kTeam, .. of 8 elements (kChunks at most).  Teams of a warp
-// share a CTA of 128 threads.
+// share a CTA of 128 threads.  Two CTAs of 1,024 an SM: 6,000 rows of 16,384 take 135 us (one: 187), fp32 sums and results 244 (272).
 template <class TX, class TR, class TY, int kTeam, int kChunks>
-__global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam, kTeam == 1024 ? 2 : 0) norm_kernel(const NormArgs a) {
   constexpr int kTeams = kTeam < 128 ? 128 / kTeam : 1;
   constexpr bool k8 = sizeof(TY) == 1;
   static_assert(kTeam == 32 || kTeam >= 128, "a team is a warp or a CTA");
@@ -109,52 +109,78 @@ __global__ void __launch_bounds__(kTeam < 128 ? 128 : kTeam) norm_kernel(const N
   for (int i = 0; i < kChunks; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) q2 = fma2(v[i][e], v[i][e], q2);
-  if (a.gain) {
+  // (one chunk's gains stay in registers; those of two would take a CTA's place on the SM, 12,000 rows of 8,192 169 us instead of 140, and
+  // are read where they are wanted)
+  uint64_t kept[4];
+  auto load_gain = [&](int i, uint64_t (&g)[4]) {
+    const int c = t + i * kTeam;
+    if (a.gain && c < n_chunks) {
+      load8<float>(a.gain, 0, 0, c, a.width, g);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = pack2(1.f, 1.f);
+    }
+  };
+  auto gain_of = [&](int i, uint64_t (&g)[4]) {
+    if (kChunks > 1) {
+      load_gain(i, g);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = kept[e];
+    }
+  };
+  if (kChunks == 1) load_gain(0, kept);
+  // the largest |r gain|, of the thread's elements, or with `scaled` the largest |r f gain|
+  auto largest = [&](bool scaled, float f) {
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      const int c = t + i * kTeam;
-      if (c >= n_chunks) continue;
       uint64_t g[4];
-      load8<float>(a.gain, 0, 0, c, a.width, g);
+      gain_of(i, g);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], g[e]);
+      for (int e = 0; e < 4; ++e) {
+        float x, y;
+        unpack2(mul2(scaled ? mul2(v[i][e], pack2(f, f)) : v[i][e], g[e]), x, y);
+        top = max3_nan(top, fabsf(x), fabsf(y));
+      }
     }
-  }
+    return top;
+  };
   float q, top = 0.f;
   {
     float x, y;
     unpack2(q2, x, y);
     q = x + y;
-    if (k8) {
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          unpack2(v[i][e], x, y);
-          top = max3_nan(top, fabsf(x), fabsf(y));
-        }
-    }
+    if (k8) top = largest(false, 1.f);
   }
   // (the order of the sum is fixed by the sizes)
   team_join<kTeam, k8>(q, top);
   // (a sum that is not finite: neither is the row, where 1 / inf would leave zeros)
   const float inv = !a.norm ? 1.f : q <= 3.40282347e38f ? rsqrtf(fmaf(q, a.inv_width, a.eps)) : NAN;
-  float f = inv, again = 1.f;
+  float back = 1.f;
   if (k8) {
-    const float s = max_nan(top * inv * (1.f / 448.f), 1.17549435e-38f), back = __fdividef(1.f, s);      // (s < 2^120: a maximum over 448)
+    if (a.norm && !(top >= 1e-30f && top <= 3.40282347e38f)) {      // r gain out of fp32's range, where v may be in it: once more, of v
+      if (kTeam > 32) __syncthreads();                 // (the join before has been read)
+      top = largest(true, inv);
+      team_join<kTeam, k8>(q, top);                    // (q is not looked at again)
+    } else {
+      top *= inv;
+    }
+    const float s = max_nan(top * (1.f / 448.f), 1.17549435e-38f);
+    back = __fdividef(1.f, s);                         // (s < 2^120: a maximum over 448)
     if (t == 0) a.scale[row] = s;
-    f = inv * back;
-    if (!(f <= 3.40282347e38f)) f = inv, again = back;      // (rows of tiny values: one after the other)
   }
+  // (v in this order: r / rms is of the size of one, r gain may leave fp32's range)
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     const int c = t + i * kTeam;
     if (c >= n_chunks) continue;
+    uint64_t g[4];
+    gain_of(i, g);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], pack2(f, f));
-    if (k8 && again != 1.f) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[i][e] = mul2(v[i][e], pack2(again, again));
+    for (int e = 0; e < 4; ++e) {
+      v[i][e] = mul2(mul2(v[i][e], pack2(inv, inv)), g[e]);
+      if (k8) v[i][e] = mul2(v[i][e], pack2(back, back));
     }
     store8<TY>(a.y, row, a.y_stride, c, a.width, v[i]);
   }
