@@ -785,22 +785,20 @@ __global__ void __launch_bounds__(kThreads, kThreads > 256 ? 1 : kAlone ? 3 : kP
     auto find = [&](const Level l, bool by_mass, bool last) {
       if (last && w_min > 1u && bin_of(floor_x) > l.bin) return;      // (min_p leaves less than the cut)
       const bool all = l.above.count + l.at.count <= (uint32_t)kList;
-      if (!all && l.at.count > (uint32_t)kList) {
-        cut_in(l, by_mass, target);
-        return;
-      }
       // (the bins have counted ids of weight alone; the last ones, and all where a difference of quotients is coarse, hold others
       // too, which could be too many: so can all of a T below 3e-38, whose first bin is wider than what has weight)
-      uint32_t own = 0u, held;
-      if (!all && last) {
-        sum_row(std::true_type{}, l.bin);
-        own = sm.n_list;
-        held = together();
-        summed = true;
-      } else {
-        held = gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+      uint32_t own = 0u, held = kList + 1;
+      if (all || l.at.count <= (uint32_t)kList) {
+        if (!all && last) {
+          sum_row(std::true_type{}, l.bin);
+          own = sm.n_list;
+          held = together();
+          summed = true;
+        } else {
+          held = gather(l.bin < 16u || fabsf(z_top) > 1e4f, [&](float x) { return all ? bin_of(x) >= l.bin : bin_of(x) == l.bin; });
+        }
       }
-      if (held > (uint32_t)kList) {                    // (the list has not come together: from the row)
+      if (held > (uint32_t)kList) {                    // (no list, or it has not come together: from the row)
         summed = false;
         cut_in(l, by_mass, target);
         return;
