@@ -513,7 +513,9 @@ cudaError_t launch8(Args8 g, const void* A, long long lda, const void* B, long l
   const long long pair_tiles = (long long)((g.M + kPairTile - 1) / kPairTile) * ((g.N + kPairTile - 1) / kPairTile);
   CUtensorMap a_map, b_map, y_map;
   if (!map_y<T>(&y_map, g)) return cudaErrorInvalidValue;
-  if (pair_tiles >= n_sm / 2) {
+  // Pairs where their tiles fill the SMs, unless few rows of B would fill a quarter of a tile at most (us, pairs against tiles of 128: 20,000 x
+  // 1 x 4,096 27.5 and 17.0, x 64 25.7 and 18.2; 131,072 x 4 x 1,024 41.3 and 28.9, x 64 33.4 and 32.8, x 128 36.8 and 39.6, x 256 as fast).
+  if (pair_tiles >= n_sm / 2 && g.N > 64) {
     if (!map8(&a_map, A, g.M, g.K, lda, kBM) || !map8(&b_map, B, g.N, g.K, ldb, kBM)) return cudaErrorInvalidValue;
     return launch_pair8<T>(g, a_map, b_map, y_map, st);
   }

@@ -30,3 +30,17 @@ def test_scales_whose_product_leaves_the_range(m, n, k, out):
         if out == "bf16" and power < 0:
             want = np.zeros_like(sums)                       # (below half of its least step, 2^-133)
         assert err.item() == 0 and np.array_equal(np64(y), want)
+
+
+@pytest.mark.parametrize("n", [1, 4, 16, 64, 65])
+def test_many_rows_of_a_for_few_of_b(n):
+    """More tiles of A than SMs, few rows of B: either side of the rule that chooses the kernel."""
+    m, k = 20000, 272
+    r = np.random.RandomState(n)
+    a, b = bytes8(r, m, k, ints=8), bytes8(r, n, k, ints=8)
+    for out in ("f32", "bf16"):
+        whole, y = strided(n, m, TYPES[out], 1, 5.0)
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        mcd.mcd_tc_gemm_e4m3(a, b, y, err)
+        want = dev(rows.gemm(np64(a), np64(b))[0], torch.float32).to(TYPES[out])
+        assert err.item() == 0 and torch.equal(y, want) and (np64(whole)[n:] == 5.0).all()
