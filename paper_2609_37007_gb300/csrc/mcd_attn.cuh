@@ -260,12 +260,13 @@ __device__ __forceinline__ void tma_page(void* dst, const CUtensorMap* map, int 
 
 // Joins the parts of `vecs` packed vectors that the CTAs of a cluster hold in the same places of their shared
 // memory: o [vec][pitch] unnormalised, m and l [vec].  Each CTA takes its share of the outputs.  A part without keys has
-// m = -inf and l = 0.
+// m = -inf and l = 0.  (The cluster's barrier wants a warp together; loops of uneven trips come before both.)
 template <class T, int D, bool kWin>
 __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, int h, const Pack& pack, int vecs, float* o, int pitch,
                                              float* m, float* l) {
   namespace cg = cooperative_groups;
   cg::cluster_group cl = cg::this_cluster();
+  __syncwarp();
   cl.sync();
   const int n = (int)cl.num_blocks(), threads = (int)blockDim.x;
   for (int t = (int)cl.block_rank() * threads + threadIdx.x; t < vecs * (D / 4); t += n * threads) {
@@ -284,6 +285,7 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, const Seq& q, in
     const float f = normaliser<kWin>(a, q, pack.row(r), sum);
     store4(static_cast<T*>(a.out) + vec_at<D>(pack, q, h, r, a.out_stride) + d, make_float4(x.x * f, x.y * f, x.z * f, x.w * f));
   }
+  __syncwarp();
   cl.sync();                                           // nobody leaves while others read
 }
 

@@ -77,6 +77,7 @@ __device__ __forceinline__ void drain(const Args8& g, const CUtensorMap* y_map, 
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         if (c + j < live && m < g.M) static_cast<T*>(g.y)[(n0 + c + j) * g.ldy + m] = v[j];
+      __syncwarp();
       continue;
     }
     T* const place = reinterpret_cast<T*>(room + turn * chunk_bytes<T>());
@@ -84,6 +85,7 @@ __device__ __forceinline__ void drain(const Args8& g, const CUtensorMap* y_map, 
     for (int j = 0; j < 32; ++j) place[j * kBM + r] = v[j];
     // (the chunk before has been read when the next is written)
     if (w == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();                                      // (barriers and loads of tensor memory want a warp together)
     fence_proxy_async();
     asm volatile("bar.sync 1, 128;" ::: "memory");
     if (w == 0 && lane == 0) {
@@ -93,6 +95,7 @@ __device__ __forceinline__ void drain(const Args8& g, const CUtensorMap* y_map, 
                      : "memory");
       asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
+    __syncwarp();
   }
 }
 // (of the thread that issued the stores: they are done)
@@ -213,6 +216,7 @@ __global__ void __launch_bounds__(kThreads8, 1)
       uint32_t turn = 0;
       drain<T>(g, &y_map, smem, turn, tmem, n0, live, m0, quarter);
       if (quarter == 0 && lane == 0) drain_done();
+      __syncwarp();
     }
   } else {
     cg::cluster_group cl = cg::this_cluster();
@@ -406,8 +410,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1)
       __syncwarp();
       if (lane == 0)
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(of_rank(smem_u32(&acc_empty[buf]), 0)) : "memory");
+      __syncwarp();
     }
     if (quarter == 0 && lane == 0) drain_done();
+    __syncwarp();
   }
   tc_fence_before();
   cl.sync();                                           // products, copies and stores of both are done
