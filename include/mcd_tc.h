@@ -56,7 +56,8 @@ mcd_status mcd_tc_gemm_tiled(int32_t M, int32_t N, int32_t K, int32_t bn, const 
  *   a_scale  dev float [M], b_scale dev float [N]; NULL: ones
  *   Y        dev [N][ldy], y_dtype MCD_WEIGHT_F32 or MCD_WEIGHT_BF16
  *   err      dev int32, zeroed by the caller: MCD_ERR_TIMEOUT if a device-side wait gave up
- * Any sizes up to 2^24, strides below 2^36 (in elements), rows 16-byte aligned (MCD_ERR_UNSUPPORTED otherwise).  Y overlaps nothing else.
+ * Any sizes up to 2^24, strides below 2^36 (in elements), rows 16-byte aligned (MCD_ERR_UNSUPPORTED otherwise).  Y and err overlap
+ * nothing (MCD_ERR_INVALID_ARG).
  * Where tiles leave SMs idle, parts of K share them, joined in a fixed order; rows do not depend on each other's values, but their last
  * bit may on N.  Asynchronous on `stream`: no allocation, no workspace, no synchronisation; can be captured. */
 mcd_status mcd_tc_gemm_e4m3(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, const float* a_scale,

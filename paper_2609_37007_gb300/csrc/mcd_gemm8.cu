@@ -549,9 +549,10 @@ extern "C" mcd_status mcd_tc_gemm_e4m3(int32_t M, int32_t N, int32_t K, const vo
   const rows::Block a{A, lda, M, K, 1}, b{B, ldb, N, K, 1}, y{Y, ldy, N, M, rows::bytes_of(y_dtype)};
   if (!a.aligned() || !b.aligned() || !y.aligned()) return MCD_ERR_UNSUPPORTED;
   if (!rows::aligned_to(a_scale, 4) || !rows::aligned_to(b_scale, 4) || !rows::aligned_to(err, 4)) return MCD_ERR_UNSUPPORTED;
-  const rows::Block sa = rows::values(a_scale, M, 4), sb = rows::values(b_scale, N, 4);
+  const rows::Block sa = rows::values(a_scale, M, 4), sb = rows::values(b_scale, N, 4), e = rows::values(err, 1, 4);
   for (const rows::Block* x : {&a, &b, &sa, &sb})
-    if (rows::overlap(y, *x)) return MCD_ERR_INVALID_ARG;
+    if (rows::overlap(y, *x) || rows::overlap(e, *x)) return MCD_ERR_INVALID_ARG;
+  if (rows::overlap(y, e)) return MCD_ERR_INVALID_ARG;
   const tc::Args8 g{a_scale, b_scale, Y, ldy, M, N, K, 0, 1, 0, err};
   // (a single row's stride is not looked at: the map wants one all the same)
   const int64_t la = M > 1 ? lda : (K + 15) / 16 * 16, lb = N > 1 ? ldb : (K + 15) / 16 * 16;
