@@ -149,7 +149,9 @@ int64_t mcd_paged_attention_workspace(const mcd_paged_kv* kv, const mcd_chunks* 
 /* mcd_paged_attention for utterances that remember their last `window` positions and their first n_sinks ones: of what
  * a row at position p sees there (cached positions and, without a mask, new rows), it keeps the positions j with
  * p - j < window or j < n_sinks.  p is the row's slot; with a mask it is cached[s] + the number of new rows that it sees - 1
- * (a drafted tree: the depth's position; a row that sees no new row: cached[s]), and which new rows it sees the mask alone says.
+ * (a drafted tree: the depth's position; a row that sees no new row: cached[s]), and which new rows it sees the mask alone says:
+ * those of a tree that is deeper than the window see ancestors from before it, as rows fed one by one would not (a row of as many
+ * bits as the window is long, or fewer, sees what they would).
  * Positions from n_sinks to cached[s] - window are seen by no row: entries of the table whose pages hold nothing else are not
  * looked at and may be -1, the pages given back.  (mcd_pages_fork and mcd_pages_compact want every page of a sequence in its
  * row of the table.)

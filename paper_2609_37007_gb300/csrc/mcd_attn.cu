@@ -2,7 +2,7 @@
 // KV head (the mathematics: mcd_attn.cuh; longer chunks: mcd_attn_chunk.cu).
 //
 // Both are built to read K and V once.  128 single rows over 17 to 1,023 keys: 50.7 us, 5.2 TB/s (fp32: 205 us, 2.6 TB/s);
-// 4 x 2 to 4 rows over up to 120,000: 245 us, 6.2 TB/s of 6.8 measured for a copy; 128 single rows with windows of 4,096 keys and 4
+// 4 x 2 to 4 rows over up to 120,000: 246 us, 6.2 TB/s of 6.8 measured for a copy; 128 single rows with windows of 4,096 keys and 4
 // sinks over up to 60,000: 344 us, 6.0 TB/s; one with a window of 1,024: 8.5 us.  fp32 chunks: 68.6 us for 24 sequences of 1
 // to 200 rows over up to 600 (4 heads of 64), a sixth of the fp32 rate: tiles of 64 rows and 64 keys are half empty, and 16
 // warps an SM (their registers) issue every other cycle (packed products, half the instructions: the same time).

@@ -16,13 +16,14 @@
 // What bounds it: a pair of tiles has 32 products of 64 cycles a key tile (D = 128; 67 measured, back to back), but
 // S to P takes a tile's softmax about 1,700 cycles (exponentials, packing and tensor memory) and its products
 // about 1,400, and the other tile fills only part of that.  The product with the first three quarters of P runs under
-// the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.27 PFLOP/s for 11,559 rows over
-// up to 8,500 keys (361 us; 0.69 of what a library product reaches; tensor pipe 55 % active).  With a window, 17,004 rows over
-// 2,048 keys and 4 sinks each: 333 us, 0.89 PFLOP/s; 18 key tiles a CTA, of which the sinks' and four at the window's ends are seen in
-// part, and 3 of them take 15 us where all else takes 1.4 us a tile.
+// the exponentials of the last (halves: 381 us): 3,200 cycles a pair, 1.32 PFLOP/s for 11,559 rows over
+// up to 8,500 keys (362 us; a library product reaches 1.92 to 1.98; tensor pipe 55 % active).  With a window, 17,004 rows over
+// 2,048 keys and 4 sinks each: 333 us, 0.89 PFLOP/s; up to 19 key tiles a CTA, of which the sinks' and two at either end of the window are
+// seen in part.  V of such a tile is looked at before its product, which takes one warp 3,200 to 3,600 cycles; a tile in the middle takes
+// 3,300 in all.
 // A CTA fills an SM, and takes about 8 us to start and end (1.5 to its place in the lists, 3 to 4 to the first scores, 2 to
 // their P, 1 to 2 to the rows of o written and the next CTA): the pairs with most keys start first (32 x 65 rows over 200 to
-// 1,500 keys: 43.9 us, in the sequences' own order 59).
+// 1,500 keys: 43.7 us, in the sequences' own order 59).
 // P is rounded to one bf16, off by 2^-8 of a probability at most, and l sums it unrounded: a hi + lo pair, as the step
 // kernel multiplies, would double the second product, half of the tensor work.  Relative to the norm of the result the
 // error is 2.2e-3 for those trees and 2.3e-3 for the long prompts; the rounding of the result alone gives 1.7e-3.
@@ -718,7 +719,7 @@ cudaError_t launch_chunk_d(AttnArgs a, cudaStream_t st) {
   while (a.splits < 8 && pairs * a.kv.n_kv_heads * a.splits * 2 <= sm_count() && keys / (2 * a.splits) >= 2 * kCTile)
     a.splits *= 2;
   // Order costs a CTA 25 ns a sequence, and what it saves is the last CTAs' time: worth it for few of either (65 rows over 200
-  // to 1,500 keys each: 32 sequences 43.9 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
+  // to 1,500 keys each: 32 sequences 43.7 us, without 59; 128, the 1,024 CTAs of 8 heads, 182 and 177).
   a.ranked = a.ch.n_seqs <= kRanked && a.ch.n_seqs * pairs * a.kv.n_kv_heads * a.splits <= 256ll * sm_count();
   // (ordered sequences leave no slots between them)
   const long long grid = (a.ranked ? pairs : slots) * a.kv.n_kv_heads * a.splits;

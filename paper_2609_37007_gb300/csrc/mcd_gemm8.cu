@@ -5,7 +5,7 @@
 // what lies behind the matrices' ends is read as zeros.
 // What bounds it: many rows the tensor cores (8,192 x 8,192 x 8,192: 304 us, 3.6 PFLOP/s; 6,144 x 8,191 x 4,096: 115 us alone, 134 in a
 // row of such calls at the power limit, tensor pipe 89 % active; one CTA a tile of 128 x 256: 438 and 183); few rows the stream of A
-// (6,144 x 4 x 4,096: 7.9 us, 3.2 TB/s) and, below about 4 us, the start of a kernel.
+// (6,144 x 4 x 4,096: 7.9 us, 3.2 TB/s; 131,072 x 4 x 4,096: 85 us, 6.3 TB/s) and, below about 4 us, the start of a kernel.
 #include <cooperative_groups.h>
 
 #include <algorithm>

@@ -17,7 +17,7 @@
 //
 // What bounds it: weights, about 30 operations each (the definition rounds every product and sum), barriers of the cluster (2,000
 // cycles each) and chains of small steps.  One row of 2,048, k = 50: 6 us on the GPU; of 131,072: 13 us, with top_p alone and 30,000
-// ids left 28 (35 of 8 rows).  128 rows of 2,048 with mixed settings 12.3 us, 96 of 131,072 (bf16) 47 to 52: as long as the rows with
+// ids left 28 (35 of 8 rows).  128 rows of 2,048 with mixed settings 12.3 us, 96 of 131,072 (bf16) 47 to 51: as long as the rows with
 // large sets, a fifth, take beside others.
 #pragma once
 #include <cooperative_groups.h>
